@@ -341,6 +341,132 @@ forge_status forge_model_decode(const forge_model_desc* model, const void* input
                                 void* stream);
 
 /* ---------------------------------------------------------------------------------------
+ * Serving a tree of drafted tokens over a (quantised) cache: rotary positions in both layouts, a
+ * cache that holds its rows in 8 bits, attention of several new tokens per sequence, and the move
+ * of the accepted branch.  One step of a serving loop verifies n drafted tokens per sequence: their rows go
+ * to cache rows p .. p + n - 1 behind the p cached ones, each attends to the cached rows and to its
+ * own ancestors, and of the accepted branch the rows are moved together.  n = 1 is the plain decode step.
+ *
+ * Common arguments.  seq_pos: DEVICE int32 [batch], cached rows of each sequence, or NULL: all
+ * have max_pos.  max_pos: HOST upper bound of seq_pos (max_pos + n <= cap); the kernels clamp every
+ * entry to [0, max_pos], as in the *_decode calls.  positions: DEVICE int32 [batch, n], the rotary
+ * position of each new row (of a draft: its depth in the tree behind seq_pos), or NULL: its cache row.
+ * n <= 64 where drafts see one another (one bit each), any length otherwise.
+ * ------------------------------------------------------------------------------------ */
+
+/* A [batch, token, head, head_dim] view of 16-bit or fp32 elements: device pointer, 16-byte aligned, and strides in
+ * elements, multiples of 8 (not looked at along an axis of one entry; 0 repeats an input); head_dim is
+ * dense.  A slice of the QKV projection's rows is such a view: no copy is needed.  HOST struct. */
+typedef struct {
+  void* ptr;
+  int64_t batch_stride, token_stride, head_stride;
+} forge_heads;
+
+typedef enum {
+  FORGE_ROPE_HALF = 0,          /* pairs (i, i + rot_dim / 2) */
+  FORGE_ROPE_INTERLEAVED = 1    /* pairs (2i, 2i + 1)         */
+} forge_rope_style;
+
+/* How the angles of a trained context are carried to a longer one.  theta_i = base^(-2i / rot_dim) radians a position,
+ * `by` the factor between the two contexts, `context` the trained one's length:
+ *   NONE    theta_i
+ *   LINEAR  theta_i / by (positions squeezed)
+ *   BASE    theta_i of the base  base * by^(rot_dim / (rot_dim - 2))
+ *   BANDS   theta_i (g + (1 - g) / by), g = clamp((turns_i - low) / (high - low), 0, 1),
+ *           turns_i = context * theta_i / 2 pi: fast pairs kept, slow ones squeezed, a blend between
+ *   RAMP    the same with g = 1 - clamp((i - first) / (last - first), 0, 1): first = floor of the (fractional) pair that
+ *           turns `high` times over the context, last = ceil of the one that turns `low` times, kept inside
+ *           [0, rot_dim - 1]; cos and sin are multiplied by 0.1 ln(by) + 1. */
+typedef enum {
+  FORGE_ROPE_SCALE_NONE = 0, FORGE_ROPE_SCALE_LINEAR = 1, FORGE_ROPE_SCALE_BASE = 2,
+  FORGE_ROPE_SCALE_BANDS = 3, FORGE_ROPE_SCALE_RAMP = 4
+} forge_rope_scaling;
+
+/* HOST function: what each pair turns a position, in units of 2^-64 of a full turn (rounded), into increments
+ * (HOST, rot_dim / 2 entries), and the factor of cos and sin.  In these units position * increment is exact modulo whole turns
+ * for every 32-bit position: there is no large angle to reduce.  context, low and high are only looked at by BANDS and RAMP.
+ * Errors: rot_dim < 2, odd or above 1024, base <= 1, by < 1, context or low <= 0, high <= low, anything not finite. */
+forge_status forge_rope_increments(double base, int rot_dim, forge_rope_scaling scaling, double by, double context,
+                                   double low, double high, uint64_t* increments, float* factor);
+
+/* The first rot_dim elements of a head turn, the others are copied.  increments: DEVICE, rot_dim / 2 entries.  HOST struct. */
+typedef struct {
+  int rot_dim;                  /* a multiple of 16 */
+  forge_rope_style style;
+  float factor;                 /* of cos and sin: finite */
+  const uint64_t* increments;
+} forge_rope_desc;
+
+/* y = rotated x, angles and products in fp32, one rounding.  y may be x itself (same strides), else the two must not overlap.
+ * Positions may be negative: the negated ones undo a rotation (by the factor's square), which is its transpose.
+ * positions is required here.  head_dim: a multiple of 16, at most 1024. */
+forge_status forge_rope_apply(const forge_rope_desc* rope, const forge_heads* x, const forge_heads* y,
+                              const int32_t* positions, int batch, int n, int heads, int head_dim,
+                              forge_dtype dt, void* stream);
+
+/* How a cache holds its rows. */
+typedef enum {
+  FORGE_KV_SAME = 0,            /* as they are, in dt */
+  FORGE_KV_INT8 = 1,            /* one fp32 scale per row: code = rint(x / scale), scale = max|x| / 127 */
+  FORGE_KV_FP8 = 2              /* e4m3 (largest value 448): code = e4m3(x / scale), scale = max|x| / 448 */
+} forge_kv_type;
+
+/* The caches of n_layers layers.  k, v: layer l, sequence b, head h, row r at element
+ * l * layer_stride + b * batch_stride + h * head_stride + r * head_dim (strides in elements, multiples of head_dim; layers,
+ * sequences and heads must not overlap); its scale at that divided by head_dim.  The 8-bit types go with dt = FORGE_BF16.
+ * Both divisions are correctly rounded fp32, codes round ties to even.  A row whose scale would be subnormal gets scale 1; a
+ * row with an infinity or NaN gets scale NaN and codes 0, and reads back as NaN.  HOST struct, device pointers. */
+typedef struct {
+  forge_kv_type type;
+  forge_dtype dt;               /* of the rows that go in and come out */
+  int n_layers, batch, kv_heads, cap, head_dim;     /* head_dim 64 or 128 */
+  int64_t layer_stride, batch_stride, head_stride;
+  void *k, *v;
+  float *k_scale, *v_scale;     /* NULL for FORGE_KV_SAME */
+} forge_kv_cache;
+
+/* New rows into layer `layer`: k rotated (rope != NULL) and v go to cache rows seq_pos[b] .. seq_pos[b] + n - 1, in the cache's
+ * type: the fp32 rotation is quantised, without a rounding to dt between.  q (NULL: none), [batch, n, q_heads, head_dim], is
+ * rotated into q_out by the same launch; q_out may be q itself. */
+forge_status forge_kv_append(const forge_kv_cache* cache, int layer, const forge_rope_desc* rope, const forge_heads* k,
+                             const forge_heads* v, const forge_heads* q, const forge_heads* q_out, int q_heads,
+                             const int32_t* seq_pos, const int32_t* positions, int n, int max_pos, void* stream);
+
+/* Rows seq_pos[b] .. seq_pos[b] + n - 1 (seq_pos NULL: max_pos .., 0 for the first n) of layer `layer`, as the values they stand
+ * for, rounded once to dt: k_out, v_out [batch, kv_heads, n, head_dim] dense, what forge_attn_fused takes. */
+forge_status forge_kv_read(const forge_kv_cache* cache, int layer, void* k_out, void* v_out, const int32_t* seq_pos, int n,
+                           int max_pos, void* stream);
+
+/* Attention of n new tokens per sequence (1 <= n <= 64) over layer `layer`, their rows already appended:
+ *   out[b, t, h*dh : (h+1)*dh] = sum_j P[b,h,t,j] v[b, g(h), j, :],  P = softmax over the rows j that t sees of scale * q . k
+ * Token t sees the cached rows j < seq_pos[b], and row seq_pos[b] + i if bit i of visible[b, t] is set (its own bit too: it is
+ * not implied).  visible: DEVICE uint64 [batch, n], or NULL: t sees the new rows 0 .. t.  A token that sees
+ * nothing gets zeros; what lies in rows that a token does not see, infinities and NaN among it, does not reach it.
+ * q: [batch, n, q_heads, head_dim]; out: [batch, n, q_heads * head_dim] dense, in dt.  fp32 scores, statistics and sums; for
+ * bf16 the weights are rounded to bf16 for the second product.  q_heads a multiple of kv_heads.
+ * The workspace size is for these lengths and every smaller max_pos. */
+size_t forge_attn_tree_workspace_bytes(const forge_kv_cache* cache, int q_heads, int n, int max_pos);
+forge_status forge_attn_tree(const forge_kv_cache* cache, int layer, const forge_heads* q, void* out,
+                             const int32_t* seq_pos, const uint64_t* visible, int q_heads, int n, int max_pos,
+                             float scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Of n new rows per sequence the accepted ones are moved together, in the caches of all layers: row seq_pos[b] + j takes row
+ * seq_pos[b] + path[b, j] for j < accepted[b].  path: DEVICE int32 [batch, n], rising (a branch from its root down);
+ * accepted: DEVICE int32 [batch], 0 .. n.  Entries outside their range are clamped.  The caller then advances seq_pos by accepted. */
+forge_status forge_kv_commit(const forge_kv_cache* cache, const int32_t* path, const int32_t* accepted,
+                             const int32_t* seq_pos, int n, int max_pos, void* stream);
+
+/* One decoder layer over n new tokens per sequence, as forge_decoder_block, with its rows in `cache` (layer `layer`):
+ * norm -> QKV projection -> forge_kv_append -> forge_attn_tree -> output projection + residual -> norm -> MLP.
+ * x_in, x_out: [batch, n, d] (may alias).  rope is given if and only if desc->use_rope; desc->rope_base is not looked at.
+ * desc and cache agree in dt, kv_heads and head_dim. */
+size_t forge_decoder_block_tree_workspace_bytes(const forge_block_desc* desc, const forge_kv_cache* cache, int n, int max_pos);
+forge_status forge_decoder_block_tree(const forge_block_desc* desc, const forge_rope_desc* rope, const forge_kv_cache* cache,
+                                      int layer, const void* x_in, void* x_out, const int32_t* seq_pos,
+                                      const int32_t* positions, const uint64_t* visible, int n, int max_pos,
+                                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
  * Static buffer plan of a flat instruction list (Sec. "Phase 4: IR Analysis & Optimization").
  * HOST functions on HOST arrays; they never touch the GPU.
  * A program has n_instr instructions over registers 0..n_regs-1: instruction j writes

@@ -20,6 +20,9 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libforge.s
 FORGE_F32, FORGE_BF16 = 0, 1
 ACT = {"none": 0, "gelu_tanh": 1, "relu": 2, "silu": 3, "swiglu": 4, "gelu_erf": 5}
 NORM = {"layernorm": 0, "rmsnorm": 1}
+KV = {"same": 0, "int8": 1, "fp8": 2}
+ROPE_STYLE = {"half": 0, "interleaved": 1}
+ROPE_SCALING = {"none": 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
 
 
 class ForgeError(RuntimeError):
@@ -40,6 +43,22 @@ class BlockDesc(C.Structure):
     ]
 
 
+class Heads(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("batch_stride", C.c_int64), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [("rot_dim", C.c_int), ("style", C.c_int), ("factor", C.c_float), ("increments", C.c_void_p)]
+
+
+class KvCache(C.Structure):
+    _fields_ = [
+        ("type", C.c_int), ("dt", C.c_int), ("n_layers", C.c_int), ("batch", C.c_int), ("kv_heads", C.c_int),
+        ("cap", C.c_int), ("head_dim", C.c_int), ("layer_stride", C.c_int64), ("batch_stride", C.c_int64),
+        ("head_stride", C.c_int64), ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+    ]
+
+
 class ModelDesc(C.Structure):
     _fields_ = [
         ("n_layers", C.c_int), ("vocab", C.c_int), ("n_pos", C.c_int), ("logits_ld", C.c_int),
@@ -52,6 +71,7 @@ _lib = None
 
 _vp, _i, _f, _sz, _i64 = C.c_void_p, C.c_int, C.c_float, C.c_size_t, C.c_int64
 _ip, _szp = C.POINTER(C.c_int), C.POINTER(C.c_size_t)
+_d, _hp, _rp, _kvp = C.c_double, C.POINTER(Heads), C.POINTER(RopeDesc), C.POINTER(KvCache)
 
 # name -> (restype, argtypes); the single list of what include/forge.h declares
 SIGNATURES = {
@@ -83,6 +103,15 @@ SIGNATURES = {
     "forge_decoder_block_decode": (_i, [C.POINTER(BlockDesc), _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _vp, _sz, _vp]),
     "forge_model_decode": (_i, [C.POINTER(ModelDesc), _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _vp, _sz, _vp]),
     "forge_compiled_bind_decode": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "forge_rope_increments": (_i, [_d, _i, _i, _d, _d, _d, _d, C.POINTER(C.c_uint64), C.POINTER(_f)]),
+    "forge_rope_apply": (_i, [_rp, _hp, _hp, _vp, _i, _i, _i, _i, _i, _vp]),
+    "forge_kv_append": (_i, [_kvp, _i, _rp, _hp, _hp, _hp, _hp, _i, _vp, _vp, _i, _i, _vp]),
+    "forge_kv_read": (_i, [_kvp, _i, _vp, _vp, _vp, _i, _i, _vp]),
+    "forge_attn_tree_workspace_bytes": (_sz, [_kvp, _i, _i, _i]),
+    "forge_attn_tree": (_i, [_kvp, _i, _hp, _vp, _vp, _vp, _i, _i, _i, _f, _vp, _sz, _vp]),
+    "forge_kv_commit": (_i, [_kvp, _vp, _vp, _vp, _i, _i, _vp]),
+    "forge_decoder_block_tree_workspace_bytes": (_sz, [C.POINTER(BlockDesc), _kvp, _i, _i]),
+    "forge_decoder_block_tree": (_i, [C.POINTER(BlockDesc), _rp, _kvp, _i, _vp, _vp, _vp, _vp, _vp, _i, _i, _vp, _sz, _vp]),
     "forge_plan_liveness": (_i, [_i, _ip, _ip, _ip, _i, _ip, _ip]),
     "forge_plan_dead_after": (_i, [_i, _ip, _i, _ip, _ip]),
     "forge_plan_linear_scan": (_i, [_i, _ip, _ip, _ip, _ip]),
@@ -409,6 +438,165 @@ def forge_model_decode(model: ModelDesc, inp, out, k_cache, v_cache, seq_pos, ma
     _check(lib().forge_model_decode(C.byref(model), _p(inp), _p(out), _p(k_cache), _p(v_cache), _p(seq_pos), B,
                                     max_pos, kv_cap, wp, wb, _stream()), "forge_model_decode")
     return out
+
+
+# ---------------------------------------------------------------------------------------------
+# Drafted trees over a (quantised) cache.
+
+
+def _heads(t: torch.Tensor) -> Heads:
+    """A [batch, token, head, head_dim] view, any strides, head_dim dense."""
+    sb, st, sh, sd = t.stride()
+    if not t.is_cuda or (sd != 1 and t.shape[3] != 1):
+        raise ValueError("forge needs [batch, token, head, head_dim] GPU tensors with a dense last axis")
+    return Heads(t.data_ptr(), sb, st, sh)
+
+
+def _int32(t: Optional[torch.Tensor], shape, what: str):
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_cuda or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous int32 GPU tensor of shape %s" % (what, tuple(shape)))
+    return t.data_ptr()
+
+
+def forge_rope_increments(base, rot_dim, scaling="none", by=1.0, context=0.0, low=1.0, high=4.0):
+    """-> (int64 CPU tensor [rot_dim / 2] of the pairs' turns a position in units of 2^-64, factor of cos and sin)."""
+    inc, factor = (C.c_uint64 * max(1, rot_dim // 2))(), C.c_float(0.0)
+    _check(lib().forge_rope_increments(base, rot_dim, ROPE_SCALING[scaling], by, context, low, high, inc, C.byref(factor)),
+           "forge_rope_increments")
+    return torch.tensor([v - (1 << 64) if v >> 63 else v for v in inc], dtype=torch.int64), factor.value
+
+
+def make_rope_desc(increments: torch.Tensor, style="half", factor=1.0) -> RopeDesc:
+    """increments: int64 GPU tensor [rot_dim / 2], kept alive on the struct."""
+    if increments.dtype != torch.int64 or not increments.is_cuda or not increments.is_contiguous():
+        raise ValueError("increments must be a contiguous int64 GPU tensor")
+    r = RopeDesc(2 * increments.numel(), ROPE_STYLE[style], factor, increments.data_ptr())
+    r._increments = increments
+    return r
+
+
+def forge_rope_apply(rope: RopeDesc, x, y, positions):
+    """y = rotated x; [B,n,H,dh] views (y may be x); positions int32 [B,n], any sign."""
+    B, n, H, dh = x.shape
+    if y.shape != x.shape or y.dtype != x.dtype:
+        raise ValueError("x and y must agree in shape and dtype")
+    _check(lib().forge_rope_apply(C.byref(rope), C.byref(_heads(x)), C.byref(_heads(y)), _int32(positions, (B, n), "positions"),
+                                  B, n, H, dh, _dt(x), _stream()), "forge_rope_apply")
+    return y
+
+
+def make_kv_cache(k, v, k_scale=None, v_scale=None) -> KvCache:
+    """k, v: [B,Hkv,cap,dh] or, of all layers, [L,B,Hkv,cap,dh] views whose rows are dense, in bf16, fp32, int8 or
+    float8_e4m3fn; the 8-bit ones with fp32 scales of the same shape and strides without dh.  The struct keeps them alive."""
+    tensors = [t for t in (k, v, k_scale, v_scale) if t is not None]
+    if k.dim() not in (4, 5) or v.shape != k.shape or v.stride() != k.stride() or v.dtype != k.dtype:
+        raise ValueError("k and v must be [B,Hkv,cap,dh] or [L,B,Hkv,cap,dh] tensors alike in shape, strides and dtype")
+    dh = k.shape[-1]
+    if any(not t.is_cuda for t in tensors) or k.stride(-1) != 1 or k.stride(-2) != dh:
+        raise ValueError("a cache holds dense rows one behind another, on the GPU")
+    c = KvCache()
+    c.type = KV[{torch.int8: "int8", torch.float8_e4m3fn: "fp8"}.get(k.dtype, "same")]
+    c.dt = FORGE_BF16 if c.type else _dt(k)
+    if (c.type != 0) != (k_scale is not None) or (k_scale is None) != (v_scale is None):
+        raise ValueError("8-bit caches, and they alone, have scales")
+    for s in (k_scale, v_scale):
+        if s is not None and (s.dtype != torch.float32 or s.shape != k.shape[:-1] or
+                              any(n > 1 and st * dh != t for n, st, t in zip(s.shape, s.stride(), k.stride()))):
+            raise ValueError("scales are fp32, shaped and strided as the rows they belong to")
+    (c.n_layers, sl), shape, stride = ((k.shape[0], k.stride(0)) if k.dim() == 5 else (1, 0)), k.shape[-4:], k.stride()[-4:]
+    c.batch, c.kv_heads, c.cap, c.head_dim = shape
+    c.layer_stride, c.batch_stride, c.head_stride = sl, stride[0], stride[1]
+    c.k, c.v = k.data_ptr(), v.data_ptr()
+    c.k_scale, c.v_scale = (None, None) if k_scale is None else (k_scale.data_ptr(), v_scale.data_ptr())
+    c._tensors = tensors
+    return c
+
+
+def _cache_dt(cache: KvCache, *tensors):
+    want = torch.float32 if cache.dt == FORGE_F32 else torch.bfloat16
+    if any(t.dtype != want for t in tensors):
+        raise ValueError("this cache takes and gives rows in %s" % want)
+
+
+def forge_kv_append(cache: KvCache, k, v, seq_pos, max_pos, rope=None, positions=None, q=None, q_out=None, layer=0):
+    """k, v [B,n,Hkv,dh] views into cache rows seq_pos[b].., k rotated; q [B,n,Hq,dh] rotated into q_out (may be q)."""
+    B, n = k.shape[:2]
+    if k.shape != (cache.batch, n, cache.kv_heads, cache.head_dim) or v.shape != k.shape:
+        raise ValueError("k and v must be [%d, n, %d, %d]" % (cache.batch, cache.kv_heads, cache.head_dim))
+    if (q is None) != (q_out is None) or (q is not None and (q.shape[:2] != (B, n) or q.shape[3] != k.shape[3] or q_out.shape != q.shape)):
+        raise ValueError("q and q_out must be [%d, %d, Hq, %d]" % (B, n, cache.head_dim))
+    _cache_dt(cache, k, v, *(() if q is None else (q, q_out)))
+    _check(lib().forge_kv_append(C.byref(cache), layer, None if rope is None else C.byref(rope), C.byref(_heads(k)),
+                                 C.byref(_heads(v)), None if q is None else C.byref(_heads(q)),
+                                 None if q is None else C.byref(_heads(q_out)), 0 if q is None else q.shape[2],
+                                 _int32(seq_pos, (B,), "seq_pos"), _int32(positions, (B, n), "positions"), n, max_pos, _stream()),
+           "forge_kv_append")
+
+
+def forge_kv_read(cache: KvCache, k_out, v_out, seq_pos=None, max_pos=0, layer=0):
+    """k_out, v_out [B,Hkv,n,dh]: rows seq_pos[b].. (seq_pos None: max_pos..) as values in the cache's activation type."""
+    B, H, n, dh = k_out.shape
+    if (B, H, dh) != (cache.batch, cache.kv_heads, cache.head_dim) or v_out.shape != k_out.shape:
+        raise ValueError("k_out and v_out must be [%d, %d, n, %d]" % (cache.batch, cache.kv_heads, cache.head_dim))
+    _cache_dt(cache, k_out, v_out)
+    _check(lib().forge_kv_read(C.byref(cache), layer, _p(k_out), _p(v_out), _int32(seq_pos, (B,), "seq_pos"), n, max_pos,
+                               _stream()), "forge_kv_read")
+    return k_out, v_out
+
+
+def forge_attn_tree_workspace_bytes(cache: KvCache, q_heads, n, max_pos) -> int:
+    return lib().forge_attn_tree_workspace_bytes(C.byref(cache), q_heads, n, max_pos)
+
+
+def _visible(t: Optional[torch.Tensor], shape):
+    if t is None:
+        return None
+    if t.dtype != torch.int64 or tuple(t.shape) != tuple(shape) or not t.is_cuda or not t.is_contiguous():
+        raise ValueError("visible must be a contiguous int64 GPU tensor of shape %s" % (tuple(shape),))
+    return t.data_ptr()
+
+
+def forge_attn_tree(cache: KvCache, q, out, seq_pos, max_pos, visible=None, scale=None, workspace=None, layer=0):
+    """q [B,n,Hq,dh] view; out [B,n,Hq*dh]; visible int64 [B,n]: bit i of entry t: new token t sees new row i (None: causal)."""
+    B, n, H, dh = q.shape
+    if B != cache.batch or dh != cache.head_dim or out.shape != (B, n, H * dh):
+        raise ValueError("q must be [%d, n, Hq, %d] and out [%d, n, Hq * %d]" % (cache.batch, cache.head_dim, cache.batch, cache.head_dim))
+    _cache_dt(cache, q, out)
+    wp, wb = _ws(workspace)
+    _check(lib().forge_attn_tree(C.byref(cache), layer, C.byref(_heads(q)), _p(out), _int32(seq_pos, (B,), "seq_pos"),
+                                 _visible(visible, (B, n)), H, n, max_pos, dh ** -0.5 if scale is None else scale, wp, wb,
+                                 _stream()), "forge_attn_tree")
+    return out
+
+
+def forge_kv_commit(cache: KvCache, path, accepted, seq_pos, max_pos):
+    """Row seq_pos[b] + j of every layer takes row seq_pos[b] + path[b, j], j < accepted[b]; path int32 [B,n], rising."""
+    B, n = path.shape
+    if B != cache.batch or accepted is None:
+        raise ValueError("path must be [%d, n], accepted [%d]" % (cache.batch, cache.batch))
+    _check(lib().forge_kv_commit(C.byref(cache), _int32(path, (B, n), "path"), _int32(accepted, (B,), "accepted"),
+                                 _int32(seq_pos, (B,), "seq_pos"), n, max_pos, _stream()), "forge_kv_commit")
+
+
+def forge_decoder_block_tree_workspace_bytes(desc: BlockDesc, cache: KvCache, n, max_pos) -> int:
+    return lib().forge_decoder_block_tree_workspace_bytes(C.byref(desc), C.byref(cache), n, max_pos)
+
+
+def forge_decoder_block_tree(desc: BlockDesc, cache: KvCache, x_in, x_out, seq_pos, max_pos, workspace, rope=None,
+                             positions=None, visible=None, layer=0):
+    """x_in / x_out [B,n,d]: one decoder layer over n new tokens per sequence, rows in `cache`."""
+    B, n, _ = x_in.shape
+    if B != cache.batch or x_out.shape != x_in.shape or x_in.shape[2] != desc.d_model:
+        raise ValueError("x_in and x_out must be [%d, n, %d]" % (cache.batch, desc.d_model))
+    _cache_dt(cache, x_in, x_out)
+    wp, wb = _ws(workspace)
+    _check(lib().forge_decoder_block_tree(C.byref(desc), None if rope is None else C.byref(rope), C.byref(cache), layer, _p(x_in),
+                                          _p(x_out), _int32(seq_pos, (B,), "seq_pos"), _int32(positions, (B, n), "positions"),
+                                          _visible(visible, (B, n)), n, max_pos, wp, wb, _stream()),
+           "forge_decoder_block_tree")
+    return x_out
 
 
 # ---------------------------------------------------------------------------------------------
