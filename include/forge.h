@@ -414,7 +414,8 @@ typedef enum {
 /* The caches of n_layers layers.  k, v: layer l, sequence b, head h, row r at element
  * l * layer_stride + b * batch_stride + h * head_stride + r * head_dim (strides in elements, multiples of head_dim; layers,
  * sequences and heads must not overlap); its scale at that divided by head_dim.  The 8-bit types go with dt = FORGE_BF16.
- * Both divisions are correctly rounded fp32, codes round ties to even.  A row whose scale would be subnormal gets scale 1; a
+ * Divisions in fp32: the scale's correctly rounded, x / scale too but for quotients within 2^-23 units of a
+ * middle between two values; codes round ties to even.  A row whose scale would be subnormal gets scale 1; a
  * row with an infinity or NaN gets scale NaN and codes 0, and reads back as NaN.  HOST struct, device pointers. */
 typedef struct {
   forge_kv_type type;

@@ -162,8 +162,14 @@ def _dt(t: torch.Tensor) -> int:
     raise ValueError("unsupported dtype %s" % t.dtype)
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream():
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    if _raw_stream is None:
+        return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    # the same handle without the Stream object around it (2.8 -> 0.2 us a call)
+    return C.c_void_p(_raw_stream(torch.cuda.current_device()))
 
 
 def _ws(t: Optional[torch.Tensor]):

@@ -38,10 +38,16 @@ __host__ __device__ inline void cos_sin(double a, float& cosine, float& sine) {
   sine = (float)(q >= 2 ? -si : si);
 }
 
-// cos and sin of `phase` 2^-64 parts of a full turn, in fp32: the nearest quarter from the top bits, the rest (the next 32 bits,
-// 2^-32 turns at most lost) in [-pi/4, pi/4], Taylor series up to x^9 / x^10 (truncated below 2e-9).  Largest error 1.2e-7.
-__host__ __device__ inline void turn_cos_sin(uint64_t phase, float& cosine, float& sine) {
-  const uint32_t top = (uint32_t)(phase >> 32);
+// The angle position * increment in units of 2^-64 turns, modulo whole turns: its top 32 bits.
+__host__ __device__ inline uint32_t turned(int32_t position, uint64_t increment) {
+  const uint32_t p = (uint32_t)position, lo = (uint32_t)increment, hi = (uint32_t)(increment >> 32);
+  const uint32_t carry = (uint32_t)((uint64_t)p * lo >> 32);
+  return p * hi + carry - (position < 0 ? lo : 0u);        // (a negative position counts 2^32 too many)
+}
+
+// cos and sin of `top` 2^-32 parts of a full turn, in fp32: the nearest quarter from the top bits, the rest in
+// [-pi/4, pi/4], Taylor series up to x^9 / x^10 (truncated below 2e-9).  Largest error 1.2e-7 with the 2^-32 turns that `turned` drops.
+__host__ __device__ inline void turn_cos_sin(uint32_t top, float& cosine, float& sine) {
   const uint32_t quarter = (top + 0x20000000u) >> 30;
   const float x = (float)(int32_t)(top - (quarter << 30)) * 1.4629180792671596e-9f;    // 2 pi / 2^32
   const float z = x * x;

@@ -19,40 +19,46 @@ __device__ inline uint32_t row_max(uint32_t v) {
   return v;
 }
 
-// One thread per 16 elements of a row and group of heads, as the rotation alone; the q heads come first, then those of k and v.
-// The row's maximum is taken over the bits of |x|: as integers they order like the values, infinities and NaN above all.
-template <typename T, forge_kv_type S, int DH>
-__global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs p, int head_groups, uint32_t total) {
+// x / scale from r = 1 / scale: the quotient by r is a few units in the last place off, a step on the exact
+// remainder leaves it correctly rounded but for quotients that lie within 2^-23 units of the middle between two values; one that
+// is a value itself, as the ties between codes are, comes out exactly.  Three instructions where the general division takes ten; the
+// remainder needs room above the subnormals.
+__device__ inline float divide(float x, float scale, float r) {
+  const float q = x * r;
+  return __builtin_fmaf(__builtin_fmaf(-q, scale, x), r, q);
+}
+
+// A thread per 16 elements of a token's rows and group of heads (blockIdx.y), as the rotation alone; the q heads come first, then
+// those of k and v.  The row's maximum is taken over the bits of |x|: as integers they order like the values, infinities and
+// NaN above all.
+template <typename T, forge_kv_type S, int DH, bool HALF>
+__global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs p, uint32_t total) {
   constexpr int ITEMS = DH / 16;
   const uint32_t gid = blockIdx.x * 256u + threadIdx.x;
   if (gid >= total) return;            // (whole rows: total is a multiple of ITEMS)
-  const uint32_t item = gid % ITEMS, rest = gid / ITEMS;
-  const uint32_t hg = rest % head_groups, tok = rest / head_groups;
-  const uint32_t b = tok / p.n, i = tok % p.n;
+  const uint32_t item = gid % ITEMS, tok = gid / ITEMS, b = tok / p.n, i = tok % p.n;
   const int nq = p.q.p != nullptr ? p.q_heads : 0, all = nq + 2 * p.kv_heads;
-  const int per = ceil_div(all, head_groups), h0 = hg * per, h1 = min(all, h0 + per);
+  const int per = ceil_div(all, gridDim.y), h0 = blockIdx.y * per, h1 = min(all, h0 + per);
   if (h0 >= h1) return;
-  const int row = first_row(p.seq_pos, b, p.max_pos) + i;
+  int64_t at_row = 0, at_scale = 0;      // of this sequence's and token's row in the first head
   Turns t = p.t;
   if (h0 >= nq + p.kv_heads) t.inc = nullptr;                 // rows of v only
-  PairTurns w(t, item, p.positions != nullptr ? p.positions[tok] : row);
-  for (int h = h0; h < h1; ++h) {
-    const bool is_q = h < nq, is_v = h >= nq + p.kv_heads;
-    const int hh = is_q ? h : is_v ? h - nq - p.kv_heads : h - nq;
-    const Heads& x = is_q ? p.q : is_v ? p.v : p.k;
-    const T* xr = reinterpret_cast<const T*>(x.p) + b * x.bs + i * x.ts + hh * x.hs;
-    // (rows of v are split as those of k: any 16 elements of the row do)
-    float a[8], c[8];
-    Vec8<T>::load(xr + w.e0, a);
-    Vec8<T>::load(xr + w.e1, c);
-    if (!is_v) w.turn(a, c);
-    if (is_q) {
-      T* yr = reinterpret_cast<T*>(p.qo.p) + b * p.qo.bs + i * p.qo.ts + hh * p.qo.hs;
+  PairTurns<HALF> w(t, item, DH);
+  auto source = [&](int h) {
+    const Heads& x = h < nq ? p.q : h < nq + p.kv_heads ? p.k : p.v;
+    const int hh = h < nq ? h : h < nq + p.kv_heads ? h - nq : h - nq - p.kv_heads;
+    return reinterpret_cast<const T*>(x.p) + b * x.bs + i * x.ts + hh * x.hs;
+  };
+  auto finish = [&](int h, float (&a)[8], float (&c)[8]) {
+    const bool is_v = h >= nq + p.kv_heads;
+    if (!is_v) w.turn(a, c);                                  // (rows of v are split as those of k: any 16 elements of the row do)
+    if (h < nq) {
+      T* yr = reinterpret_cast<T*>(p.qo.p) + b * p.qo.bs + i * p.qo.ts + h * p.qo.hs;
       Vec8<T>::store(yr + w.e0, a);
       Vec8<T>::store(yr + w.e1, c);
-      continue;
+      return;
     }
-    const int64_t e = b * p.c.bs + hh * p.c.hs + (int64_t)row * DH;
+    const int64_t head = (is_v ? h - nq - p.kv_heads : h - nq) * p.c.hs, e = head + at_row;
     char* cache = is_v ? p.c.v : p.c.k;
     if constexpr (S == FORGE_KV_SAME) {
       T* yr = reinterpret_cast<T*>(cache) + e;
@@ -64,21 +70,39 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs p, int head_g
       for (int j = 0; j < 8; ++j) m = max(m, max(__float_as_uint(a[j]) & 0x7fffffffu, __float_as_uint(c[j]) & 0x7fffffffu));
       m = row_max<ITEMS>(m);
       const bool finite = m < 0x7f800000u;
-      float scale = __fdiv_rn(__uint_as_float(m), Codes<S>::top);
+      float scale = divide(__uint_as_float(m), Codes<S>::top, 1.f / Codes<S>::top);      // (an infinity: NaN)
       if (scale < 1.17549435e-38f) scale = 1.f;
       if (!finite) scale = __uint_as_float(0x7fc00000u);
+      float by = scale, r;
+      if (__any(!finite || scale < 1e-30f)) {                 // (rare)
+        const float k = !finite ? 0.f : scale < 1e-30f ? 18446744073709551616.f : 1.f;       // room below, by a power of two
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          a[j] = finite ? a[j] * k : 0.f;
+          c[j] = finite ? c[j] * k : 0.f;
+        }
+        by = finite ? scale * k : 1.f;
+      }
+      r = __builtin_amdgcn_rcpf(by);
+      r = __builtin_fmaf(__builtin_fmaf(-by, r, 1.f), r, r);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        a[j] = finite ? __fdiv_rn(a[j], scale) : 0.f;
-        c[j] = finite ? __fdiv_rn(c[j], scale) : 0.f;
+        a[j] = divide(a[j], by, r);
+        c[j] = divide(c[j], by, r);
       }
       const u32x2 lo = {Codes<S>::pack(a[0], a[1], a[2], a[3]), Codes<S>::pack(a[4], a[5], a[6], a[7])};
       const u32x2 hi = {Codes<S>::pack(c[0], c[1], c[2], c[3]), Codes<S>::pack(c[4], c[5], c[6], c[7])};
       *reinterpret_cast<u32x2*>(cache + e + w.e0) = lo;
       *reinterpret_cast<u32x2*>(cache + e + w.e1) = hi;
-      if (item == 0) (is_v ? p.c.vs : p.c.ks)[e / DH] = scale;
+      if (item == 0) (is_v ? p.c.vs : p.c.ks)[head / DH + at_scale] = scale;
     }
-  }
+  };
+  walk_heads<T>(h0, h1, w.e0, w.e1, source, [&] {
+    const int row = first_row(p.seq_pos, b, p.max_pos) + i;
+    at_row = b * p.c.bs + (int64_t)row * DH;
+    at_scale = at_row / DH;
+    w.at(t, p.positions != nullptr ? p.positions[tok] : row);
+  }, finish);
 }
 
 // Rows back as values: a thread per 8 elements; grid (rows of one head in blocks, heads of k and v, batch)
@@ -120,11 +144,10 @@ __global__ __launch_bounds__(64) void kv_commit_kernel(CacheView c, int64_t laye
   char* rows = (is_v ? c.v : c.k) + blockIdx.z * layer_bytes + b * bs_bytes + h * hs_bytes + (int64_t)pos * ROW_BYTES;
   float* scales = is_v ? c.vs : c.ks;
   if (scales != nullptr) scales += blockIdx.z * layer_rows + b * bs_rows + h * hs_rows + pos;
+  const int mine = min(max(lane < n ? path[(int64_t)b * n + lane] : 0, 0), n - 1);      // n <= 64: an entry a lane
   for (int j0 = 0; j0 < take; j0 += ROWS) {
-    const int j = j0 + lane / LANES;
-    if (j >= take) break;
-    const int from = min(max(path[(int64_t)b * n + j], 0), n - 1);
-    if (from == j) continue;
+    const int j = j0 + lane / LANES, from = __shfl(mine, j & 63, 64);
+    if (j >= take || from == j) continue;
     const u32x4 x = *reinterpret_cast<const u32x4*>(rows + (int64_t)from * ROW_BYTES + lane % LANES * 16);
     float s = 0.f;
     if (scales != nullptr && lane % LANES == 0) s = scales[from];
@@ -134,9 +157,10 @@ __global__ __launch_bounds__(64) void kv_commit_kernel(CacheView c, int64_t laye
 }
 
 template <typename T, forge_kv_type S>
-void append_dh(const AppendArgs& a, unsigned blocks, int groups, uint32_t total, hipStream_t s) {
-  if (a.head_dim == 64) kv_append_kernel<T, S, 64><<<blocks, 256, 0, s>>>(a, groups, total);
-  else kv_append_kernel<T, S, 128><<<blocks, 256, 0, s>>>(a, groups, total);
+void append_dh(const AppendArgs& a, const dim3& grid, uint32_t total, hipStream_t s) {
+  auto go = [&](auto kernel) { kernel<<<grid, 256, 0, s>>>(a, total); };
+  if (a.head_dim == 64) a.t.half ? go(kv_append_kernel<T, S, 64, true>) : go(kv_append_kernel<T, S, 64, false>);
+  else a.t.half ? go(kv_append_kernel<T, S, 128, true>) : go(kv_append_kernel<T, S, 128, false>);
 }
 
 template <typename T, forge_kv_type S>
@@ -151,14 +175,13 @@ void read_dh(const CacheView& c, int batch, int kv_heads, int head_dim, void* k_
 
 forge_status launch_kv_append(const AppendArgs& a, hipStream_t s) {
   const int heads = (a.q.p != nullptr ? a.q_heads : 0) + 2 * a.kv_heads;
-  const int64_t base = (int64_t)a.batch * a.n * (a.head_dim / 16);
-  const int groups = row_head_groups(base, heads);
-  const int64_t total = base * groups;
+  const int64_t total = (int64_t)a.batch * a.n * (a.head_dim / 16);
   const unsigned blocks = (unsigned)ceil_div64(total, 256);
-  if (a.dt == FORGE_F32) append_dh<float, FORGE_KV_SAME>(a, blocks, groups, (uint32_t)total, s);
-  else if (a.type == FORGE_KV_SAME) append_dh<bf16, FORGE_KV_SAME>(a, blocks, groups, (uint32_t)total, s);
-  else if (a.type == FORGE_KV_INT8) append_dh<bf16, FORGE_KV_INT8>(a, blocks, groups, (uint32_t)total, s);
-  else append_dh<bf16, FORGE_KV_FP8>(a, blocks, groups, (uint32_t)total, s);
+  const dim3 grid(blocks, row_head_groups(blocks, heads));
+  if (a.dt == FORGE_F32) append_dh<float, FORGE_KV_SAME>(a, grid, (uint32_t)total, s);
+  else if (a.type == FORGE_KV_SAME) append_dh<bf16, FORGE_KV_SAME>(a, grid, (uint32_t)total, s);
+  else if (a.type == FORGE_KV_INT8) append_dh<bf16, FORGE_KV_INT8>(a, grid, (uint32_t)total, s);
+  else append_dh<bf16, FORGE_KV_FP8>(a, grid, (uint32_t)total, s);
   return launch_status();
 }
 

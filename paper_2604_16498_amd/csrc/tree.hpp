@@ -43,7 +43,7 @@ struct TreeArgs {
   void* out;
   const int* seq_pos;
   const uint64_t* visible;
-  int batch, n, q_heads, kv_heads, head_dim, max_pos;
+  int batch, n, q_heads, kv_heads, head_dim, max_pos, cap;
   float scale;
   forge_kv_type type;
   forge_dtype dt;
@@ -60,15 +60,18 @@ forge_status launch_kv_commit(const CacheView& c, forge_kv_type type, forge_dtyp
                               const int* seq_pos, int n, int max_pos, hipStream_t s);
 forge_status launch_attn_tree(const TreeArgs& a, hipStream_t s);
 // serves every smaller max_pos too
-size_t attn_tree_workspace_bytes(int batch, int q_heads, int kv_heads, int head_dim, int n, int max_pos, bool f32);
+size_t attn_tree_workspace_bytes(int batch, int q_heads, int kv_heads, int head_dim, int n, int max_pos, int cap, bool f32);
 
 // codes <-> fp32.  The largest code of a row's type, and four codes a word.
 template <forge_kv_type T> struct Codes;
 template <> struct Codes<FORGE_KV_INT8> {
   static constexpr float top = 127.f;
+  // of values up to 127 (1 + 2^-23) in magnitude: in x + 1.5 * 2^23 the sum is rounded to a whole number, ties to even, whose two's
+  // complement is the low byte
   static __device__ inline uint32_t pack(float a, float b, float c, float d) {
-    auto q = [](float x) { return (uint32_t)(int)rintf(fminf(fmaxf(x, -127.f), 127.f)) & 0xffu; };
-    return q(a) | q(b) << 8 | q(c) << 16 | q(d) << 24;
+    auto q = [](float x) { return __float_as_uint(x + 12582912.f); };
+    const uint32_t lo = __builtin_amdgcn_perm(q(b), q(a), 0x0c0c0400), hi = __builtin_amdgcn_perm(q(d), q(c), 0x04000c0c);
+    return lo | hi;
   }
   static __device__ inline void unpack(uint32_t w, float* f) {
 #pragma unroll
@@ -77,9 +80,9 @@ template <> struct Codes<FORGE_KV_INT8> {
 };
 template <> struct Codes<FORGE_KV_FP8> {
   static constexpr float top = 448.f;
+  // of values up to 448 (1 + 2^-23) in magnitude, which is rounded to 448
   static __device__ inline uint32_t pack(float a, float b, float c, float d) {
-    auto q = [](float x) { return fminf(fmaxf(x, -448.f), 448.f); };
-    return __builtin_amdgcn_cvt_pk_fp8_f32(q(c), q(d), __builtin_amdgcn_cvt_pk_fp8_f32(q(a), q(b), 0, false), true);
+    return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
   }
   static __device__ inline void unpack(uint32_t w, float* f) {
     const floatx2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);

@@ -82,7 +82,7 @@ forge_status check_tree(const forge_kv_cache* c, int layer, int q_heads, int n, 
 struct TreeBlockPlan {
   size_t y, qkv, o, u, attn, gemm, total;
 };
-TreeBlockPlan plan_tree_block(const forge_block_desc* d, int batch, int n, int max_pos) {
+TreeBlockPlan plan_tree_block(const forge_block_desc* d, int batch, int n, int max_pos, int cap) {
   const size_t es = esize(d->dt), T = (size_t)batch * n;
   const int hd = d->q_heads * d->head_dim, nqkv = (d->q_heads + 2 * d->kv_heads) * d->head_dim, rows = (int)T;
   const bool w8 = block_w8(d);
@@ -91,7 +91,7 @@ TreeBlockPlan plan_tree_block(const forge_block_desc* d, int batch, int n, int m
   p.qkv = align_up(T * nqkv * es, 256);
   p.o = align_up(T * hd * es, 256);
   p.u = block_mlp_bytes(d, T);
-  p.attn = align_up(attn_tree_workspace_bytes(batch, d->q_heads, d->kv_heads, d->head_dim, n, max_pos, d->dt == FORGE_F32), 256);
+  p.attn = align_up(attn_tree_workspace_bytes(batch, d->q_heads, d->kv_heads, d->head_dim, n, max_pos, cap, d->dt == FORGE_F32), 256);
   p.gemm = 0;
   for (size_t v : {gemm_ws(rows, nqkv, d->d_model, FORGE_ACT_NONE, d->dt, w8, true),
                    gemm_ws(rows, d->d_model, hd, FORGE_ACT_NONE, d->dt, w8),
@@ -213,7 +213,7 @@ forge_status forge_kv_read(const forge_kv_cache* cache, int layer, void* k_out, 
 
 size_t forge_attn_tree_workspace_bytes(const forge_kv_cache* cache, int q_heads, int n, int max_pos) {
   if (check_cache(cache) != FORGE_OK || check_tree(cache, 0, q_heads, n, max_pos) != FORGE_OK) return 0;
-  return attn_tree_workspace_bytes(cache->batch, q_heads, cache->kv_heads, cache->head_dim, n, max_pos, cache->dt == FORGE_F32);
+  return attn_tree_workspace_bytes(cache->batch, q_heads, cache->kv_heads, cache->head_dim, n, max_pos, cache->cap, cache->dt == FORGE_F32);
 }
 
 forge_status forge_attn_tree(const forge_kv_cache* cache, int layer, const forge_heads* q, void* out, const int32_t* seq_pos,
@@ -227,10 +227,10 @@ forge_status forge_attn_tree(const forge_kv_cache* cache, int layer, const forge
       !bits_ok(visible) || !scale_ok(scale))
     return FORGE_ERR_INVALID_ARG;
   if (out == q->ptr || out == cache->k || out == cache->v) return FORGE_ERR_INVALID_ARG;
-  const size_t need = attn_tree_workspace_bytes(B, q_heads, cache->kv_heads, cache->head_dim, n, max_pos, cache->dt == FORGE_F32);
+  const size_t need = attn_tree_workspace_bytes(B, q_heads, cache->kv_heads, cache->head_dim, n, max_pos, cache->cap, cache->dt == FORGE_F32);
   if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return FORGE_ERR_WORKSPACE;
   TreeArgs a = {layer_of(cache, layer), view(q, B, n, q_heads), out, seq_pos, visible, B, n, q_heads, cache->kv_heads,
-                cache->head_dim, max_pos, scale, cache->type, cache->dt, workspace};
+                cache->head_dim, max_pos, cache->cap, scale, cache->type, cache->dt, workspace};
   return launch_attn_tree(a, static_cast<hipStream_t>(stream));
 }
 
@@ -251,7 +251,7 @@ size_t forge_decoder_block_tree_workspace_bytes(const forge_block_desc* desc, co
   if (check_block_desc(desc) != FORGE_OK || check_cache(cache) != FORGE_OK || !fits(desc, cache) ||
       check_tree(cache, 0, desc->q_heads, n, max_pos) != FORGE_OK)
     return 0;
-  return plan_tree_block(desc, cache->batch, n, max_pos).total;
+  return plan_tree_block(desc, cache->batch, n, max_pos, cache->cap).total;
 }
 
 forge_status forge_decoder_block_tree(const forge_block_desc* desc, const forge_rope_desc* rope, const forge_kv_cache* cache,
@@ -268,7 +268,7 @@ forge_status forge_decoder_block_tree(const forge_block_desc* desc, const forge_
   if (!req(x_in) || !req(x_out) || !req(workspace) || !int_ptr_ok(seq_pos) || !int_ptr_ok(positions) || !bits_ok(visible))
     return FORGE_ERR_INVALID_ARG;
   const int B = cache->batch, T = B * n, dm = desc->d_model, dh = desc->head_dim, hq = desc->q_heads, hkv = desc->kv_heads;
-  const TreeBlockPlan pl = plan_tree_block(desc, B, n, max_pos);
+  const TreeBlockPlan pl = plan_tree_block(desc, B, n, max_pos, cache->cap);
   if (workspace_bytes < pl.total) return FORGE_ERR_WORKSPACE;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const forge_dtype dt = desc->dt;
@@ -293,7 +293,7 @@ forge_status forge_decoder_block_tree(const forge_block_desc* desc, const forge_
   if (rope == nullptr) ap.q.p = nullptr;
   st = launch_kv_append(ap, s);
   if (st != FORGE_OK) return st;
-  TreeArgs at = {ap.c, part(0), o, seq_pos, visible, B, n, hq, hkv, dh, max_pos, 1.0f / sqrtf((float)dh), cache->type, dt, aws};
+  TreeArgs at = {ap.c, part(0), o, seq_pos, visible, B, n, hq, hkv, dh, max_pos, cache->cap, 1.0f / sqrtf((float)dh), cache->type, dt, aws};
   st = launch_attn_tree(at, s);
   if (st != FORGE_OK) return st;
   // (decode-sized: the reduce step of the projection also produces the second norm)

@@ -19,7 +19,10 @@ SHIM = """
 #define __device__
 #include "%s"
 extern "C" void turn_all(const unsigned long* p, float* c, float* s, long n) {
-  for (long i = 0; i < n; ++i) forge::turn_cos_sin(p[i], c[i], s[i]);
+  for (long i = 0; i < n; ++i) forge::turn_cos_sin(p[i] >> 32, c[i], s[i]);
+}
+extern "C" void turned_all(const int* p, const unsigned long* inc, unsigned* top, long n) {
+  for (long i = 0; i < n; ++i) top[i] = forge::turned(p[i], inc[i]);
 }
 """
 
@@ -42,6 +45,13 @@ def test_turns_to_cos_and_sin(tmp_path):
     # the angle: half a unit of fp32 at pi/4 twice (conversion, product) and 2^-32 turns; the series: three roundings near 1
     bound = 2 * 2.0**-25 + 2 * math.pi * 2.0**-32 + 3 * 2.0**-25
     assert max(np.abs(c - np.cos(angle)).max(), np.abs(s - np.sin(angle)).max()) <= bound
+    # positions of any sign: the top of the product modulo 2^64
+    p = np.concatenate([rng.integers(-2**31, 2**31, 100000), [0, 1, -1, 2**31 - 1, -2**31]]).astype(np.int32)
+    inc = rng.integers(0, 2**64, p.size, dtype=np.uint64)
+    top = np.empty(p.size, np.uint32)
+    C.CDLL(str(lib)).turned_all(ptr(p), ptr(inc), ptr(top), C.c_long(p.size))
+    want = np.array([int(a) * int(b) % 2**64 >> 32 for a, b in zip(p, inc)], np.uint32)
+    np.testing.assert_array_equal(top, want)
 
 
 @pytest.mark.parametrize("scaling", list(B.ROPE_SCALING))
