@@ -169,7 +169,7 @@ def _stream():
     if _raw_stream is None:
         return C.c_void_p(torch.cuda.current_stream().cuda_stream)
     # the same handle without the Stream object around it (2.8 -> 0.2 us a call)
-    return C.c_void_p(_raw_stream(torch.cuda.current_device()))
+    return _raw_stream(torch._C._cuda_getDevice())
 
 
 def _ws(t: Optional[torch.Tensor]):
@@ -461,7 +461,7 @@ def _heads(t: torch.Tensor) -> Heads:
 def _int32(t: Optional[torch.Tensor], shape, what: str):
     if t is None:
         return None
-    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_cuda or not t.is_contiguous():
+    if t.dtype != torch.int32 or t.shape != shape or not t.is_cuda or not t.is_contiguous():
         raise ValueError("%s must be a contiguous int32 GPU tensor of shape %s" % (what, tuple(shape)))
     return t.data_ptr()
 
@@ -522,8 +522,9 @@ def make_kv_cache(k, v, k_scale=None, v_scale=None) -> KvCache:
 
 def _cache_dt(cache: KvCache, *tensors):
     want = torch.float32 if cache.dt == FORGE_F32 else torch.bfloat16
-    if any(t.dtype != want for t in tensors):
-        raise ValueError("this cache takes and gives rows in %s" % want)
+    for t in tensors:
+        if t.dtype != want:
+            raise ValueError("this cache takes and gives rows in %s" % want)
 
 
 def forge_kv_append(cache: KvCache, k, v, seq_pos, max_pos, rope=None, positions=None, q=None, q_out=None, layer=0):
@@ -559,7 +560,7 @@ def forge_attn_tree_workspace_bytes(cache: KvCache, q_heads, n, max_pos) -> int:
 def _visible(t: Optional[torch.Tensor], shape):
     if t is None:
         return None
-    if t.dtype != torch.int64 or tuple(t.shape) != tuple(shape) or not t.is_cuda or not t.is_contiguous():
+    if t.dtype != torch.int64 or t.shape != shape or not t.is_cuda or not t.is_contiguous():
         raise ValueError("visible must be a contiguous int64 GPU tensor of shape %s" % (tuple(shape),))
     return t.data_ptr()
 

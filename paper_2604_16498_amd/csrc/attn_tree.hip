@@ -111,7 +111,6 @@ template <> struct Store<FORGE_KV_SAME, bf16> {
     f[0] = bf_lo(w[0]); f[1] = bf_hi(w[0]); f[2] = bf_lo(w[1]); f[3] = bf_hi(w[1]);
   }
 };
-__device__ inline uint32_t pack_pair(float a, float b) { return pack_bf2(a, b); }
 template <> struct Store<FORGE_KV_INT8, bf16> {
   static constexpr int BYTES = 1;
   static __device__ inline float byte(uint32_t w, int i) { return (float)(int8_t)(w >> (8 * i)); }
@@ -120,14 +119,14 @@ template <> struct Store<FORGE_KV_INT8, bf16> {
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       const uint32_t w = r.k[f][j / 2][2 * (j & 1) + t / 2];
-      o[t] = pack_pair(byte(w, 2 * (t & 1)), byte(w, 2 * (t & 1) + 1));
+      o[t] = pack_bf2(byte(w, 2 * (t & 1)), byte(w, 2 * (t & 1) + 1));
     }
     return __builtin_bit_cast(bf16x8, o);
   }
   template <int DH> static __device__ inline u32x4 v(const Raw<1, DH>& r, int m) {
     u32x4 o;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) o[t] = pack_pair(byte(r.v[2 * t][m / 4], m & 3), byte(r.v[2 * t + 1][m / 4], m & 3));
+    for (int t = 0; t < 4; ++t) o[t] = pack_bf2(byte(r.v[2 * t][m / 4], m & 3), byte(r.v[2 * t + 1][m / 4], m & 3));
     return o;
   }
   static __device__ inline int q_at(int j, int kg) { return 64 * (j / 2) + 16 * kg + 8 * (j & 1); }
@@ -983,14 +982,16 @@ __global__ __launch_bounds__(256) void attn_tree_merge(TreeParams p, int block_r
 // over `alone` cache rows per us, the blocks of a full CU together over `full`, the memory gives 6.2 MB; to the largest of the three (a cubic
 // mean: they add a little) comes 1 us for every block per CU, and for shares the merge launch of 2.3 us, the partials at 4.2 MB per us and
 // 1.4 us for every pair a share has on the average.  Of a ragged batch 0.63 of the longest cache is taken for the mean, a guess: the
-// host does not know the lengths.  Fitted to 500 drawn calls timed at every choice (heads of 64 and 128, 1 to 64 sequences, 1 to 64 tokens): the
-// choice is 1.4 % off the best in the geometric mean, 29 % at most; without the 1 us it was 2.2 % and 61 %.  us, whole | 256 shares | 512:
+// host does not know the lengths.  The numbers were fitted so that the choices come out, not each time: 1100 drawn calls of more than 16 query
+// rows (heads of 64 and 128, 1 to 64 sequences, 3 to 64 tokens) timed at every choice; of the 200 that had no part in the fit the choice is
+// 1.3 % off the best in the geometric mean, 19 % at most.  us, whole | 256 shares | 512:
 // 7 sequences up to 4984 rows of 16 heads of 128, 5 tokens 56.8 | 39.7 | 40.4, 62 up to 137 of 8 x 4, 10 tokens, blocks of 128 rows
-// 15.8 | 27.5 | 26.5, of 32 rows 25.4 | 35.9 | 29.2, 18 up to 3309 of 8 x 4, 40 tokens, of 256 rows 106 | 69.7 | -, of 128 rows 96 | 88 | 74.
+// 15.8 | 27.5 | 26.5, of 32 rows 25.4 | 35.9 | 29.2, 16 up to 8191 of 8 x 4, 64 tokens, of 256 rows 195 | 124 | -, of 128 rows 167 | 145 | 133,
+// of 32 rows 181 | 221 | 181.
 struct TreePlan { int block_rows, row_blocks, shares, dealt; };
 struct TreeSpeed { int block_rows; float alone[2], full[2]; };      // rows per us, heads of 128: 8 bits, 16 bits
-constexpr TreeSpeed kSpeeds[] = {{16, {190.f, 200.f}, {4000.f, 430.f}}, {32, {100.f, 118.f}, {100.f, 90.f}},
-                                 {128, {42.f, 54.f}, {63.f, 60.f}}, {256, {30.f, 40.f}, {19.f, 26.f}}};
+constexpr TreeSpeed kSpeeds[] = {{16, {190.f, 200.f}, {4000.f, 430.f}}, {32, {150.f, 167.f}, {105.f, 86.f}},
+                                 {128, {51.f, 60.f}, {54.f, 54.f}}, {256, {35.f, 40.f}, {133.f, 52.f}}};
 constexpr int MIN_CUT_ROWS = 512;         // a shorter cache is never dealt, so its calls need no workspace
 
 // whether a call may run on blocks of this many query rows (fp32 and few rows: the smallest; a cache of less than one tile: not on
@@ -1015,13 +1016,13 @@ TreePlan plan_tree(int batch, int q_heads, int kv_heads, int head_dim, int n, in
   const bool f32 = element_bytes == 4;
   const double pairs = (double)batch * kv_heads, mean = (ragged && batch > 1 ? 0.63 : 1.0) * len, cus = compute_units();
   const double mb = pairs * mean * 2.0 * (head_dim * element_bytes + (wide ? 0 : 4)) * 1e-6;
-  const double narrow = (head_dim == 64 ? 1.6 : 1.0) * (f32 ? 0.4 : 1.0);
   TreePlan best = {};
   double least = 0.0;
   for (const TreeSpeed& v : kSpeeds) {
     if (!tree_rows_ok(v.block_rows, rows, cap, f32)) continue;
     const int rb = ceil_div(rows, v.block_rows);
-    const double alone = v.alone[wide] * narrow, full = v.full[wide] * narrow;
+    const double by = (head_dim == 128 ? 1.0 : v.block_rows == 16 ? 1.6 : v.block_rows == 32 ? 1.8 : 1.5) * (f32 ? 0.4 : 1.0);
+    const double alone = v.alone[wide] * by, full = v.full[wide] * by;
     for (int per_cu = 0; per_cu <= (v.block_rows == 256 ? 1 : 2); ++per_cu) {      // 0: whole pairs
       if (per_cu > 0 && !tree_may_deal(batch, (int64_t)batch * kv_heads, len)) break;
       const int shares = per_cu > 0 ? tree_shares((int64_t)batch * kv_heads, len, rb, per_cu) : batch * kv_heads;

@@ -67,9 +67,10 @@ CacheView layer_of(const forge_kv_cache* c, int layer) {
           c->batch > 1 ? c->batch_stride : 0, c->kv_heads > 1 ? c->head_stride : 0};
 }
 
+// the attention's blocks, a (sequence, cache head) and 16 query rows each, rounded up to whole turns of the XCDs, are a 32-bit grid
 bool tree_sizes_ok(const forge_kv_cache* c, int q_heads, int n) {
   return q_heads <= kMaxGridDim && rows_ok(c->batch, n) &&
-         (int64_t)c->batch * c->kv_heads * kMaxDrafts * 8 * ceil_div(q_heads / c->kv_heads * n, 16) < ((int64_t)1 << 31);
+         ((int64_t)c->batch * c->kv_heads + 8) * ceil_div(q_heads / c->kv_heads * n, 16) < ((int64_t)1 << 24);
 }
 
 forge_status check_tree(const forge_kv_cache* c, int layer, int q_heads, int n, int max_pos) {
