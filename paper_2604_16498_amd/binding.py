@@ -529,17 +529,24 @@ def _cache_dt(cache: KvCache, *tensors):
 
 def forge_kv_append(cache: KvCache, k, v, seq_pos, max_pos, rope=None, positions=None, q=None, q_out=None, layer=0):
     """k, v [B,n,Hkv,dh] views into cache rows seq_pos[b].., k rotated; q [B,n,Hq,dh] rotated into q_out (may be q)."""
-    B, n = k.shape[:2]
-    if k.shape != (cache.batch, n, cache.kv_heads, cache.head_dim) or v.shape != k.shape:
+    shape = k.shape
+    B, n, heads, dh = shape
+    if B != cache.batch or heads != cache.kv_heads or dh != cache.head_dim or v.shape != shape:
         raise ValueError("k and v must be [%d, n, %d, %d]" % (cache.batch, cache.kv_heads, cache.head_dim))
-    if (q is None) != (q_out is None) or (q is not None and (q.shape[:2] != (B, n) or q.shape[3] != k.shape[3] or q_out.shape != q.shape)):
-        raise ValueError("q and q_out must be [%d, %d, Hq, %d]" % (B, n, cache.head_dim))
-    _cache_dt(cache, k, v, *(() if q is None else (q, q_out)))
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out come together")
+    if q is None:
+        q_heads, qp, qop = 0, None, None
+        _cache_dt(cache, k, v)
+    else:
+        q_heads = q.shape[2]
+        if q.shape != (B, n, q_heads, dh) or q_out.shape != q.shape:
+            raise ValueError("q and q_out must be [%d, %d, Hq, %d]" % (B, n, dh))
+        _cache_dt(cache, k, v, q, q_out)
+        qp, qop = C.byref(_heads(q)), C.byref(_heads(q_out))
     _check(lib().forge_kv_append(C.byref(cache), layer, None if rope is None else C.byref(rope), C.byref(_heads(k)),
-                                 C.byref(_heads(v)), None if q is None else C.byref(_heads(q)),
-                                 None if q is None else C.byref(_heads(q_out)), 0 if q is None else q.shape[2],
-                                 _int32(seq_pos, (B,), "seq_pos"), _int32(positions, (B, n), "positions"), n, max_pos, _stream()),
-           "forge_kv_append")
+                                 C.byref(_heads(v)), qp, qop, q_heads, _int32(seq_pos, (B,), "seq_pos"),
+                                 _int32(positions, (B, n), "positions"), n, max_pos, _stream()), "forge_kv_append")
 
 
 def forge_kv_read(cache: KvCache, k_out, v_out, seq_pos=None, max_pos=0, layer=0):

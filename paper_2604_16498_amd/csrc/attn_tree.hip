@@ -248,7 +248,9 @@ struct Deal {
     return b;
   }
 };
-// the first unit of share i, and the share that holds unit x
+// The shares that the units are dealt over: of a batch that is shorter than the host had to expect no more than units, so that none between
+// two shares of a pair is empty.  The first unit of share i, and the share that holds unit x:
+__device__ inline uint32_t shares_of(const TreeParams& p, uint32_t units) { return min((uint32_t)p.shares, units); }
 __device__ inline uint32_t share_begin(uint32_t i, uint32_t units, uint32_t shares) { return (uint32_t)((uint64_t)i * units / shares); }
 __device__ inline uint32_t share_of(uint32_t x, uint32_t units, uint32_t shares) {
   return (uint32_t)((((uint64_t)x + 1) * shares - 1) / units);       // the largest i with floor(i units / shares) <= x
@@ -298,9 +300,10 @@ struct Share {
       left = 0x7fffffffu;
     } else {
       const Deal d(p);
-      const uint32_t all = d.total * p.kv_heads, x = share_begin(i, all, p.shares);
-      left = uniform(share_begin(i + 1, all, p.shares) - x);
-      if (left == 0) return false;
+      const uint32_t all = d.total * p.kv_heads, shares = shares_of(p, all);
+      if ((uint32_t)i >= shares) return false;
+      const uint32_t x = share_begin(i, all, shares);
+      left = uniform(share_begin(i + 1, all, shares) - x);
       b = uniform(d.holder(x, p.kv_heads));
       uint32_t first, count;
       d.of(b, first, count);
@@ -943,7 +946,8 @@ __global__ __launch_bounds__(256) void attn_tree_merge(TreeParams p, int block_r
   uint32_t first, count;
   deal.of(b, first, count);
   const uint32_t all = deal.total * p.kv_heads, x = first * p.kv_heads + g * count;
-  const int i0 = share_of(x, all, p.shares), i1 = share_of(x + count - 1, all, p.shares);
+  const uint32_t shares = shares_of(p, all);
+  const int i0 = share_of(x, all, shares), i1 = share_of(x + count - 1, all, shares);
   if (i0 == i1 || row >= p.rows) return;
   const int rb = row / block_rows, r = row % block_rows;
   float mx = -FLT_MAX, l = 0.f;

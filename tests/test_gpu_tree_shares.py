@@ -1,0 +1,97 @@
+"""Attention of drafted trees where its work is cut in other ways: many sequences, one long among short ones, whole pairs and shares, blocks of
+every size, caches without a row to spare.  Against fp64 on the device; all rows that no token sees hold NaN."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2604_16498_amd import binding as F
+from tree_inputs import ancestor_bits, cache_arrays, gpu, normal, parents, signed
+
+pytestmark = pytest.mark.gpu
+
+STORES = ["int8", "fp8", "bf16", "fp32"]
+
+
+def lengths(rng, B, top, kind):
+    if kind == "one long":
+        pos = rng.integers(0, 50, B)
+        pos[B // 3] = top
+    elif kind == "alike":
+        pos = np.full(B, top)
+    else:
+        pos = rng.integers(0, top + 1, B)
+        pos[rng.integers(0, B)] = top
+    return [int(p) for p in pos]
+
+
+def check_call(rng, store, B, n, Hq, Hkv, dh, pos, max_pos=None, spare=3):
+    max_pos = max(pos) if max_pos is None else max_pos
+    cap = max_pos + n + spare
+    (k, v, ks, vs), _ = cache_arrays(rng, store, (B, Hkv, cap, dh))
+    seen = torch.arange(cap, device="cuda")[None] < torch.tensor(pos, device="cuda")[:, None] + n
+    dead = ~seen[:, None, :].expand(B, Hkv, cap)
+    for t in (ks, vs) if store in ("int8", "fp8") else (k, v):
+        t[dead] = float("nan")
+    if store == "fp8":
+        for t in (k, v):
+            t.view(torch.uint8)[dead] = 0x7f
+    dt = torch.float32 if store == "fp32" else torch.bfloat16
+    q = gpu(normal(rng, (B, n, Hq, dh), store != "fp32"), dt)
+    vis = [ancestor_bits(parents(rng, n)) for _ in range(B)]
+    c = F.make_kv_cache(k, v, ks, vs)
+    ws = F.workspace(F.forge_attn_tree_workspace_bytes(c, Hq, n, max_pos))
+    if ws is not None:
+        ws.fill_(255)                                             # NaN wherever it is read before it is written
+    out = torch.full((B, n, Hq * dh), 7.0, dtype=dt, device="cuda")
+    bits = torch.tensor(signed(vis), dtype=torch.int64, device="cuda")
+    F.forge_attn_tree(c, q, out, torch.tensor(pos, dtype=torch.int32, device="cuda"), max_pos, visible=bits, workspace=ws)
+    G = Hq // Hkv
+    for b, p in enumerate(pos):
+        rows = p + n
+        kk, vv = ((t[b, :, :rows].float().double() * (1.0 if s is None else s[b, :, :rows, None].double())) for t, s in ((k, ks), (v, vs)))
+        qq = q[b].double().view(n, Hkv, G, dh).permute(1, 2, 0, 3).reshape(Hkv, G * n, dh)
+        s = torch.matmul(qq, kk.transpose(1, 2).contiguous()) * dh ** -0.5
+        draft = torch.arange(rows, device="cuda") - p
+        ok = (draft[None] < 0) | ((bits[b][:, None] >> draft.clamp(min=0)[None]) & 1).bool()
+        s = s.view(Hkv, G, n, rows).masked_fill(~ok, -torch.inf).softmax(-1).view(Hkv, G * n, rows)
+        want, size = (torch.matmul(s, x).view(Hkv, G, n, dh).permute(2, 0, 1, 3).reshape(n, Hq * dh) for x in (vv, vv.abs()))
+        err = (out[b].double() - want).abs()
+        # 16-bit: weights and output are rounded to bf16, 2^-8 of sum P |v| each; scores and sums in fp32 add about 1e-5
+        bound = 2e-5 * size + 1e-5 if store == "fp32" else (2 * 2.0 ** -8 * 1.02 + 2e-5) * size + 1e-6
+        assert (err <= bound).all(), (b, p, float((err - bound).max()))        # (false for NaN)
+
+
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("B,n,Hq,Hkv,dh,top,kind", [
+    (300, 3, 4, 2, 64, 700, "ragged"), (256, 1, 2, 1, 128, 900, "ragged"), (257, 2, 2, 1, 64, 600, "ragged"), (65, 1, 8, 8, 64, 800, "ragged"),
+    (64, 1, 8, 8, 128, 1000, "ragged"), (48, 8, 16, 8, 128, 700, "ragged"), (40, 1, 4, 1, 128, 6000, "one long"), (40, 12, 8, 2, 64, 6000, "one long"),
+    (9, 20, 8, 1, 128, 4000, "one long"), (7, 5, 3, 3, 128, 2500, "alike"), (70, 9, 4, 1, 128, 1100, "ragged"), (100, 40, 4, 1, 64, 600, "ragged")])
+def test_cut_over_sequences(B, n, Hq, Hkv, dh, top, kind, store):
+    rng = np.random.default_rng(B + n)
+    check_call(rng, store, B, n, Hq, Hkv, dh, lengths(rng, B, top, kind))
+
+
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("B,n,Hq,Hkv,dh,top", [
+    (1, 64, 8, 1, 128, 3000), (3, 33, 8, 1, 64, 5000), (20, 64, 6, 1, 128, 513), (2, 64, 5, 1, 128, 1025), (5, 26, 12, 2, 64, 1500),
+    (130, 40, 4, 1, 128, 520), (33, 50, 16, 2, 64, 640), (1, 63, 17, 1, 128, 2049)])
+def test_many_query_rows(B, n, Hq, Hkv, dh, top, store):
+    rng = np.random.default_rng(B + n + 1)
+    check_call(rng, store, B, n, Hq, Hkv, dh, lengths(rng, B, top, "ragged"))
+
+
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("B,n,Hq,Hkv,dh,pos", [
+    (1, 1, 1, 1, 64, [0]), (2, 1, 8, 2, 128, [3, 0]), (2, 5, 4, 1, 64, [10, 26]), (1, 31, 4, 2, 128, [0]), (1, 16, 3, 1, 128, [16]), (2, 64, 2, 1, 64, [0, 63]),
+    (3, 7, 4, 4, 128, [600, 0, 999]), (4, 24, 4, 1, 128, [1000, 31, 32, 33])])
+def test_no_row_to_spare(B, n, Hq, Hkv, dh, pos, store):
+    """cap is the last row of the longest sequence, also below one tile"""
+    check_call(np.random.default_rng(n), store, B, n, Hq, Hkv, dh, pos, spare=0)
+
+
+@pytest.mark.parametrize("store", ["int8", "bf16"])
+def test_a_workspace_serves_shorter_lengths(store):
+    """positions far below max_pos: the cut is made for longer ones, and there are fewer rows than shares"""
+    for n in (1, 40):
+        for pos in ([0, 5, 130], [0, 0, 0], [300, 2000, 1]):
+            check_call(np.random.default_rng(n), store, 3, n, 8, 2, 128, pos, max_pos=6000)
