@@ -95,3 +95,39 @@ def test_a_workspace_serves_shorter_lengths(store):
     for n in (1, 40):
         for pos in ([0, 5, 130], [0, 0, 0], [300, 2000, 1]):
             check_call(np.random.default_rng(n), store, 3, n, 8, 2, 128, pos, max_pos=6000)
+
+
+@pytest.mark.parametrize("store", ["fp8", "bf16", "fp32"])
+@pytest.mark.parametrize("n,Hq,pos", [(40, 8, [3000, 10]), (64, 6, [700, 130]), (12, 8, [5000, 3])])
+def test_an_infinity_reaches_those_that_see_it(n, Hq, pos, store):
+    """one element of one draft's v; every other output keeps its bits"""
+    rng = np.random.default_rng(n)
+    dh, Hkv, at, col = 128, 2, 7, 5
+    dt = torch.float32 if store == "fp32" else torch.bfloat16
+    (k, v, ks, vs), _ = cache_arrays(rng, store, (2, Hkv, max(pos) + n, dh))
+    vis = [ancestor_bits(parents(rng, n)) for _ in range(2)]
+    q = gpu(normal(rng, (2, n, Hq, dh), store != "fp32"), dt)
+    c = F.make_kv_cache(k, v, ks, vs)
+    ws = F.workspace(F.forge_attn_tree_workspace_bytes(c, Hq, n, max(pos)))
+    bits, seq = torch.tensor(signed(vis), dtype=torch.int64, device="cuda"), torch.tensor(pos, dtype=torch.int32, device="cuda")
+    outs = []
+    for spoil in (False, True):
+        if spoil:
+            for b, p in enumerate(pos):
+                if store == "fp8":
+                    v.view(torch.uint8)[b, 1, p + at, col] = 0xff        # NaN: the type has no infinity
+                else:
+                    v[b, 1, p + at, col] = float("-inf")
+        out = torch.empty(2, n, Hq * dh, dtype=dt, device="cuda")
+        F.forge_attn_tree(c, q, out, seq, max(pos), visible=bits, workspace=ws)
+        outs.append(out.view(2, n, Hkv, Hq // Hkv, dh))
+    hit = torch.zeros_like(outs[0], dtype=torch.bool)
+    for b in range(2):
+        for t in range(n):
+            hit[b, t, 1, :, col] = bool(vis[b][t] >> at & 1)
+    # (the element itself counts as 0 among the rest of its column)
+    same = outs[0] == outs[1]
+    column = torch.zeros_like(hit)
+    column[:, :, 1, :, col] = True
+    assert same[~column].all() and same[column & ~hit].all() and hit.any()
+    assert (torch.isnan(outs[1][hit]) if store == "fp8" else outs[1][hit] == float("-inf")).all()
