@@ -3,20 +3,23 @@
 //
 // The G = Hq / Hkv query heads of a cache head and the n tokens are one set of G n query rows (row = token * G + head), taken in
 // tiles of 16.  A block of 4 waves owns RT such tiles of one (sequence, cache head) and one range of cache rows; its waves take
-// the 32-row tiles of the range in turn, and nothing but the final merge goes through LDS:
-//   scores   S^T = K . Q^T (v_mfma_f32_16x16x32_bf16): K rows are the A operand, loaded from memory in its layout, 16 bytes a
-//            lane (the order of the contraction is free, Q follows it).  Row r of the 16-row half f of a tile is cache row
+// the 32-row tiles of the range in turn, each through a patch of LDS that no other wave touches, and meet only to add up:
+//   scores   S^T = K . Q^T (v_mfma_f32_16x16x32_bf16): K rows are the A operand, 16 bytes a lane and read
+//            (the order of the contraction is free, Q follows it).  Row r of the 16-row half f of a tile is cache row
 //            8 (r / 4) + r % 4 + 4 f, so that a lane ends up with the scores of 8 consecutive cache rows for its query row ...
 //   softmax  ... and with their weights as the B operand of the second product, without moving them.  Running maximum per
 //            query row, held back until a tile exceeds it by 2^8 (fp32 sums have room for that, and rescaling becomes rare).
-//   P . V    O^T = V^T . P^T: the lane that holds columns c (DH / 16) .. of its 8 cache rows, loaded in whole
-//            pieces of the rows, forms the transposed operand with the packing that the conversion needs anyway.
+//   P . V    O^T = V^T . P^T: the lane that reads columns c (DH / 16) .. of its 8 cache rows
+//            forms the transposed operand with the packing that the conversion needs anyway.
 // Rows in 8 bits become bf16 exactly (int8 and e4m3 both fit its 8 significant bits); their scales multiply the scores
 // and the weights in fp32.  fp32 caches run the same way on v_mfma_f32_16x16x4_f32, all operands in fp32.
-// More than 32 query rows: attn_tree_wide_kernel below, whose waves share the cache rows through LDS.
-// The rows of all (sequence, cache head) pairs are dealt evenly over the blocks in units of 128, whatever the lengths, which only
-// the device knows: every block finds its share from the positions.  A pair that one block holds whole is
+// Many query rows: attn_tree_wide_kernel below, whose waves share the cache rows through LDS.
+// The rows of all (sequence, cache head) pairs are dealt evenly over the blocks in units of 128 where that is estimated to pay, whatever the lengths,
+// which only the device knows: every block finds its share from the positions.  A pair that one block holds whole is
 // finished there; of the others fp32 partials go to the workspace and a second kernel merges them in order.  No atomics.
+// Measured, 32 heads over 8 of 128: one token, 64 sequences up to 2049 rows, int8 (174 MB) 37 us, 4.7 TB/s: memory.  26 tokens, 5 up to 8217 rows, fp8
+// 32 + 6 us, 0.34 PFLOP/s; 64 tokens, 16 up to 8255, bf16 107 + 12 us, 0.8 PFLOP/s: a SIMD's matrix and vector cycles, which add up whichever
+// of its waves they come from, then the partials.  One token, 334 rows of 12 heads of 64: 5.8 us, a chain of loads.
 #include <float.h>
 #include <math.h>
 #include "tree.hpp"
@@ -47,7 +50,7 @@ struct TreeParams {
 };
 
 // ---- how cache rows become matrix operands -------------------------------------------------------------------
-// Raw: the registers of a 32-row tile.  k[f]: rows of half f in the A layout (lane = row l % 16, 16 bytes per 64 contiguous
+// Raw: the operands of a 32-row tile.  k[f]: rows of half f in the A layout (lane = row l % 16, 16 bytes per 64 contiguous
 // ones); v[i]: columns c (DH / 16) .. of row 8 (l / 16) + i, c = l % 16.
 // Neither layout is read from memory: a wave-wide load of 16 rows x 16 bytes a quarter costs a line lookup per lane, and the
 // lookups, not the bytes, then bound the kernel (int8, 64 ragged sequences up to 2049 rows of 8 heads: 45 us, the address unit
@@ -655,7 +658,7 @@ __global__ __launch_bounds__(NW * 64, RT == 1 && sizeof(T) == 2 && (S != FORGE_K
   }
 }
 
-// ---- more than 32 query rows -----------------------------------------------------------------------------------
+// ---- many query rows -------------------------------------------------------------------------------------------
 // A block of WAVES waves owns 32 query rows a wave and walks over its cache rows in tiles of KT, which come from memory through
 // registers into LDS as bf16 (8-bit rows are converted once per block there), two buffers each of K and V: a tile is stored
 // while the one before it is multiplied, and requested a tile earlier still.  v_mfma_f32_32x32x16_bf16: S^T = K . Q^T with a query row
