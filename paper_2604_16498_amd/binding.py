@@ -151,7 +151,7 @@ def _p(t: Optional[torch.Tensor]):
         return None
     if not t.is_cuda or not t.is_contiguous():
         raise ValueError("forge tensors must be contiguous GPU tensors")
-    return C.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _dt(t: torch.Tensor) -> int:
@@ -173,7 +173,7 @@ def _stream():
 
 
 def _ws(t: Optional[torch.Tensor]):
-    return (_p(t), 0 if t is None else t.numel() * t.element_size())
+    return (None, 0) if t is None else (_p(t), t.nbytes)
 
 
 def _check(status: int, where: str):
