@@ -286,15 +286,17 @@ struct Share {
   int b, g, unit;       // where the next piece begins
   int pos;              // of sequence b; a vector register, not waited for before the piece is taken
   // false: nothing to do.  Blocks go round-robin over the 8 XCDs: those of one share are 8 apart, so that its rows come into one L2
-  __device__ inline bool start(const TreeParams& p) {
+  // A block (or, of `of` shares a block, this wave)
+  __device__ inline bool start(const TreeParams& p, int of = 1, int wave = 0) {
     i = blockIdx.x;
     rb = 0;
     if (p.row_blocks > 1) {
       const int turn = blockIdx.x / (8 * p.row_blocks), in = blockIdx.x % (8 * p.row_blocks);
       i = turn * 8 + in % 8;
       rb = in / 8;
-      if (i >= p.shares) return false;
     }
+    i = i * of + wave;
+    if (i >= p.shares) return false;
     unit = 0;
     if (!p.dealt) {
       const int at = p.by_length > 0 ? by_length(p, i) : i;
@@ -375,7 +377,8 @@ __device__ inline uint64_t wave_marks(uint64_t mine) {
   return all;
 }
 
-template <forge_kv_type S, typename T, int DH, int RT>
+// EACH: pairs are not cut, and every wave takes one by itself; nothing is added up between waves.
+template <forge_kv_type S, typename T, int DH, int RT, bool EACH>
 __global__ __launch_bounds__(NW * 64, RT == 1 && sizeof(T) == 2 && (S != FORGE_KV_SAME || DH == 64) ? 3 : 2) void attn_tree_kernel(TreeParams p) {
   typedef Store<S, T> St;
   constexpr int BYTES = St::BYTES;
@@ -390,9 +393,11 @@ __global__ __launch_bounds__(NW * 64, RT == 1 && sizeof(T) == 2 && (S != FORGE_K
   __shared__ float sml[NW][16][2];
   __shared__ uint64_t oddbuf[NW];
 
-  Share share;
-  if (!share.start(p)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  constexpr int SIDE = EACH ? 1 : NW;                          // waves side by side in a range of rows
+  const int beside = EACH ? 0 : wave;
+  Share share;
+  if (!share.start(p, EACH ? NW : 1, EACH ? wave : 0)) return;
   const int c = lane & 15, kg = lane >> 4;
   char* const lds = patch[wave];
 
@@ -404,7 +409,7 @@ __global__ __launch_bounds__(NW * 64, RT == 1 && sizeof(T) == 2 && (S != FORGE_K
   u32x4 rk[L::LOADS], rv[L::LOADS];                            // the tile in flight
   float rs = 0.f;
   int begin = 0;
-  auto tile_base = [&](int t) { return begin + (t * NW + wave) * TILE; };
+  auto tile_base = [&](int t) { return begin + (t * SIDE + beside) * TILE; };
   // Tiles are read whole: one that passes the end of the cache from the cache's last rows instead (those that belong to
   // the tile before are cut below), what lies between the end of the sequence and that is cut too.  So the addresses of a tile are one
   // scalar base and constant offsets.  (fp32: each piece clamped, so that a cache may be shorter than a tile)
@@ -472,7 +477,7 @@ __global__ __launch_bounds__(NW * 64, RT == 1 && sizeof(T) == 2 && (S != FORGE_K
   for (;;) {
   const Piece at = share.next(p);
   const int pos = at.pos, stop = at.stop;
-  const int ntile = stop > begin + wave * TILE ? ceil_div(stop - begin - wave * TILE, NW * TILE) : 0;
+  const int ntile = stop > begin + beside * TILE ? ceil_div(stop - begin - beside * TILE, SIDE * TILE) : 0;
   marks = 0;
   float m_run[RT], l_run[RT];
   floatx4 acc[RT][NM];
@@ -624,17 +629,19 @@ __global__ __launch_bounds__(NW * 64, RT == 1 && sizeof(T) == 2 && (S != FORGE_K
         *reinterpret_cast<floatx4*>(lds + c * (PAD * 4) + ((4 * kg + v) * NM + m) * 4) =
             floatx4{acc[i][m][v], acc[i][m + 1][v], acc[i][m + 2][v], acc[i][m + 3][v]};
     if (kg == 0) { sml[wave][c][0] = m_run[i]; sml[wave][c][1] = l; }
-    lds_barrier();
-    for (int idx = tid; idx < 16 * (DH / 4); idx += NW * 64) {
+    if constexpr (EACH) wave_lds_sync();
+    else lds_barrier();
+    for (int idx = EACH ? lane : tid; idx < 16 * (DH / 4); idx += SIDE * 64) {
       const int r = idx / (DH / 4), d = idx % (DH / 4) * 4, row = (share.rb * RT + i) * 16 + r;
       if (row >= p.rows) continue;
-      float mn = sml[0][r][0];
+      const int w0 = EACH ? wave : 0;
+      float mn = sml[w0][r][0];
 #pragma unroll
-      for (int w = 1; w < NW; ++w) mn = fmaxf(mn, sml[w][r][0]);
+      for (int w = 1; w < SIDE; ++w) mn = fmaxf(mn, sml[w][r][0]);
       floatx4 o = {0.f, 0.f, 0.f, 0.f};
       float lt = 0.f;
 #pragma unroll
-      for (int w = 0; w < NW; ++w) {
+      for (int w = w0; w < w0 + SIDE; ++w) {
         const float a = __builtin_amdgcn_exp2f(sml[w][r][0] - mn);
         o += *reinterpret_cast<const floatx4*>(patch[w] + r * (PAD * 4) + d * 4) * a;
         lt += sml[w][r][1] * a;
@@ -642,7 +649,7 @@ __global__ __launch_bounds__(NW * 64, RT == 1 && sizeof(T) == 2 && (S != FORGE_K
       if constexpr (S != FORGE_KV_INT8) {
         uint64_t odd = 0;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) odd |= oddbuf[w];
+        for (int w = w0; w < w0 + SIDE; ++w) odd |= oddbuf[w];
         if (odd != 0) put_back<St, DH>(p, at.b, row / p.group, odd, v_rows, pos, d, o);
       }
       if (at.which < 0) {
@@ -652,7 +659,7 @@ __global__ __launch_bounds__(NW * 64, RT == 1 && sizeof(T) == 2 && (S != FORGE_K
         if (d == 0) { p.stat[(slot + 16 * i + r) * 2] = mn; p.stat[(slot + 16 * i + r) * 2 + 1] = lt; }
       }
     }
-    lds_barrier();
+    if constexpr (!EACH) lds_barrier();
   }
   if (!more) break;
   }
@@ -995,7 +1002,7 @@ __global__ __launch_bounds__(256) void attn_tree_merge(TreeParams p, int block_r
 // 7 sequences up to 4984 rows of 16 heads of 128, 5 tokens 56.8 | 39.7 | 40.4, 62 up to 137 of 8 x 4, 10 tokens, blocks of 128 rows
 // 15.8 | 27.5 | 26.5, of 32 rows 25.4 | 35.9 | 29.2, 16 up to 8191 of 8 x 4, 64 tokens, of 256 rows 195 | 124 | -, of 128 rows 167 | 145 | 133,
 // of 32 rows 181 | 221 | 181.
-struct TreePlan { int block_rows, row_blocks, shares, dealt; };
+struct TreePlan { int block_rows, row_blocks, shares, dealt, each; };
 struct TreeSpeed { int block_rows; float alone[2], full[2]; };      // rows per us, heads of 128: 8 bits, 16 bits
 constexpr TreeSpeed kSpeeds[] = {{16, {190.f, 200.f}, {4000.f, 430.f}}, {32, {150.f, 167.f}, {105.f, 86.f}},
                                  {128, {51.f, 60.f}, {54.f, 54.f}}, {256, {35.f, 40.f}, {133.f, 52.f}}};
@@ -1040,19 +1047,27 @@ TreePlan plan_tree(int batch, int q_heads, int kv_heads, int head_dim, int n, in
         us += 2.3 + (shares + pairs) * rb * fmin(v.block_rows, rows) * head_dim * 8e-6 / 4.2 + 1.4 * pairs / shares;
       if (best.block_rows == 0 || us < least) {
         least = us;
-        best = {v.block_rows, rb, shares, per_cu > 0};
+        best = {v.block_rows, rb, shares, per_cu > 0, 0};
       }
     }
   }
+  // A short cache has fewer tiles than a block waves; where blocks have to wait for others, a wave per pair instead.  us, a block | a
+  // wave a pair, one token: 55 x 12 pairs of 64 up to 22 rows 9.0 | 4.9, 64 x 8 of 128 up to 28 8.7 | 5.7, 99 x 8 up to 82 14.0 | 10.2; time of the
+  // wave against the block's: 1 to 2 pairs a CU up to 96 rows 0.7 to 0.95, up to 256 1.0 to 1.2; more pairs up to 192 rows 0.65 to 0.95, up to 400 1.0 to 1.1.
+  // (rows in tiles of 32: 0.8 to 1.6, so not there)
+  const int64_t blocks = (int64_t)best.shares * best.row_blocks;
+  best.each = best.block_rows == 16 && !best.dealt && blocks > compute_units() && len <= (blocks > 2 * compute_units() ? 192 : 96);
   return best;
 }
 
 template <forge_kv_type S, typename T, int DH>
 void launch_blocks(const TreeParams& p, const TreePlan& pl, hipStream_t s) {
-  const unsigned blocks = pl.row_blocks > 1 ? (unsigned)(ceil_div(pl.shares, 8) * 8 * pl.row_blocks) : (unsigned)pl.shares;
-  if (pl.block_rows == 16) attn_tree_kernel<S, T, DH, 1><<<blocks, NW * 64, 0, s>>>(p);
+  const int apart = pl.each ? ceil_div(pl.shares, NW) : pl.shares;
+  const unsigned blocks = pl.row_blocks > 1 ? (unsigned)(ceil_div(apart, 8) * 8 * pl.row_blocks) : (unsigned)apart;
+  if (pl.block_rows == 16 && pl.each) attn_tree_kernel<S, T, DH, 1, true><<<blocks, NW * 64, 0, s>>>(p);
+  if (pl.block_rows == 16 && !pl.each) attn_tree_kernel<S, T, DH, 1, false><<<blocks, NW * 64, 0, s>>>(p);
   if constexpr (sizeof(T) == 2) {
-    if (pl.block_rows == 32) attn_tree_kernel<S, T, DH, 2><<<blocks, NW * 64, 0, s>>>(p);
+    if (pl.block_rows == 32) attn_tree_kernel<S, T, DH, 2, false><<<blocks, NW * 64, 0, s>>>(p);
     // (8-bit rows of 64: a tile of 64 rows is less than a piece for each of 8 waves' threads)
     constexpr int KT8 = S != FORGE_KV_SAME && DH == 64 ? 128 : 64;
     if (pl.block_rows == 128) attn_tree_wide_kernel<S, DH, 4, 64><<<blocks, 4 * 64, 0, s>>>(p);
@@ -1110,9 +1125,10 @@ forge_status launch_attn_tree(const TreeArgs& a, hipStream_t s) {
   p.dealt = pl.dealt;
   // Whole pairs by length where some CU gets a second block (us, in batch order | by length, 64 sequences up to 2001 rows of 8 heads of 128: 8 tokens
   // 16 bits 72.3 | 70.0, int8 52.9 | 50.8, 48 of them 46.4 | 42.0, 21 up to 1401 of 16 heads, one token 36.8 | 32.4)
-  const int64_t blocks = (int64_t)pl.shares * pl.row_blocks;
+  const int apart = pl.each ? NW : 1;
+  const int64_t blocks = (int64_t)ceil_div(pl.shares, apart) * pl.row_blocks;
   p.by_length = !pl.dealt && a.seq_pos != nullptr && a.batch > 1 && a.batch <= 64 && blocks > compute_units() && pl.row_blocks <= compute_units()
-                    ? compute_units() / pl.row_blocks : 0;
+                    ? compute_units() / pl.row_blocks * apart : 0;
   p.row_blocks = pl.row_blocks;
   p.scale_log2e = a.scale * 1.4426950408889634f;
   p.part = (float*)a.workspace;

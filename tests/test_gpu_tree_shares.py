@@ -131,3 +131,38 @@ def test_an_infinity_reaches_those_that_see_it(n, Hq, pos, store):
     column[:, :, 1, :, col] = True
     assert same[~column].all() and same[column & ~hit].all() and hit.any()
     assert (torch.isnan(outs[1][hit]) if store == "fp8" else outs[1][hit] == float("-inf")).all()
+
+
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("B,n,Hq,Hkv,dh,top", [
+    (50, 1, 12, 12, 64, 20), (100, 4, 12, 4, 128, 60), (65, 3, 16, 8, 64, 190), (400, 2, 2, 1, 128, 31), (33, 16, 8, 8, 128, 70), (37, 5, 21, 7, 128, 32)])
+def test_many_short_caches(B, n, Hq, Hkv, dh, top, store):
+    rng = np.random.default_rng(B + n + 2)
+    check_call(rng, store, B, n, Hq, Hkv, dh, lengths(rng, B, top, "ragged"), spare=int(rng.integers(0, 3)) + 8 * (top < 31))
+
+
+@pytest.mark.parametrize("store", ["fp8", "bf16", "fp32"])
+def test_an_infinity_in_short_caches(store):
+    """drafts see their own row alone among the new ones; every second sequence's second draft holds an infinity (fp8: NaN)"""
+    rng = np.random.default_rng(12)
+    B, n, H, dh = 60, 3, 8, 64
+    dt = torch.float32 if store == "fp32" else torch.bfloat16
+    pos = [int(p) for p in rng.integers(0, 41, B)]
+    (k, v, ks, vs), _ = cache_arrays(rng, store, (B, H, 64, dh))
+    q = gpu(normal(rng, (B, n, H, dh), store != "fp32"), dt)
+    c = F.make_kv_cache(k, v, ks, vs)
+    bits, seq = torch.tensor([[1, 2, 4]] * B, dtype=torch.int64, device="cuda"), torch.tensor(pos, dtype=torch.int32, device="cuda")
+    outs = []
+    for spoil in (False, True):
+        for b in range(0, B if spoil else 0, 2):
+            if store == "fp8":
+                v.view(torch.uint8)[b, :, pos[b] + 1, 9] = 0x7f
+            else:
+                v[b, :, pos[b] + 1, 9] = float("inf")
+        out = torch.empty(B, n, H * dh, dtype=dt, device="cuda")
+        F.forge_attn_tree(c, q, out, seq, max(pos), visible=bits, workspace=F.workspace(F.forge_attn_tree_workspace_bytes(c, H, n, max(pos))))
+        outs.append(out.view(B, n, H, dh))
+    hit = torch.zeros_like(outs[0], dtype=torch.bool)
+    hit[::2, 1, :, 9] = True
+    assert torch.equal(outs[0][~hit], outs[1][~hit])
+    assert (torch.isnan(outs[1][hit]) if store == "fp8" else outs[1][hit] == float("inf")).all()
