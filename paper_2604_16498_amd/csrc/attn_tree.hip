@@ -947,11 +947,14 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_tree_wide_kernel(TreeParam
 }
 
 // The shares of a query row in order, 4 a round trip: DH / 4 lanes a row.  Rows that one share held whole are there already.
-template <typename T, int DH>
+// SPLIT: all lanes of the block for one row, the shares in as many runs, added in their order at the end (32 shares a pair, 4 rows of 8 pairs: 8 -> 4 us).
+template <typename T, int DH, bool SPLIT>
 __global__ __launch_bounds__(256) void attn_tree_merge(TreeParams p, int block_rows) {
   constexpr int LPR = DH / 4, PER = 256 / LPR;
+  __shared__ floatx4 so[SPLIT ? PER : 1][LPR];
+  __shared__ float sm[SPLIT ? PER : 1][2];
   const int pair = blockIdx.y, b = pair / p.kv_heads, g = pair % p.kv_heads;
-  const int row = blockIdx.x * PER + threadIdx.x / LPR, d = threadIdx.x % LPR * 4;
+  const int run = threadIdx.x / LPR, row = SPLIT ? blockIdx.x : blockIdx.x * PER + run, at = threadIdx.x % LPR, d = at * 4;
   const Deal deal(p);
   uint32_t first, count;
   deal.of(b, first, count);
@@ -960,18 +963,20 @@ __global__ __launch_bounds__(256) void attn_tree_merge(TreeParams p, int block_r
   const int i0 = share_of(x, all, shares), i1 = share_of(x + count - 1, all, shares);
   if (i0 == i1 || row >= p.rows) return;
   const int rb = row / block_rows, r = row % block_rows;
+  const int each = SPLIT ? ceil_div(i1 - i0 + 1, PER) : 0;
+  const int from = SPLIT ? min(i0 + run * each, i1 + 1) : i0, to = SPLIT ? min(from + each, i1 + 1) : i1 + 1;
   float mx = -FLT_MAX, l = 0.f;
   floatx4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int z0 = i0; z0 <= i1; z0 += 4) {
+  for (int z0 = from; z0 < to; z0 += 4) {
     float mz[4], lz[4];
     floatx4 oz[4];
 #pragma unroll
     for (int z = 0; z < 4; ++z) {
-      const int i = min(z0 + z, i1);
-      const int64_t at = slot_of(p, i, rb, i == i0, block_rows) + r;
-      mz[z] = p.stat[at * 2];
-      lz[z] = p.stat[at * 2 + 1];
-      oz[z] = *reinterpret_cast<const floatx4*>(p.part + at * DH + d);
+      const int i = min(z0 + z, to - 1);
+      const int64_t slot = slot_of(p, i, rb, i == i0, block_rows) + r;
+      mz[z] = p.stat[slot * 2];
+      lz[z] = p.stat[slot * 2 + 1];
+      oz[z] = *reinterpret_cast<const floatx4*>(p.part + slot * DH + d);
     }
     float mn = mx;
 #pragma unroll
@@ -982,11 +987,29 @@ __global__ __launch_bounds__(256) void attn_tree_merge(TreeParams p, int block_r
     o *= a;
 #pragma unroll
     for (int z = 0; z < 4; ++z)
-      if (z0 + z <= i1) {
+      if (z0 + z < to) {
         const float w = __builtin_amdgcn_exp2f(mz[z] - mn);
         l += lz[z] * w;
         o += oz[z] * w;
       }
+  }
+  if constexpr (SPLIT) {
+    so[run][at] = o;
+    if (at == 0) { sm[run][0] = mx; sm[run][1] = l; }
+    __syncthreads();
+    if (run > 0) return;
+    float top = mx;
+#pragma unroll
+    for (int w = 1; w < PER; ++w) top = fmaxf(top, sm[w][0]);
+    const float a = __builtin_amdgcn_exp2f(mx - top);
+    l *= a;
+    o *= a;
+#pragma unroll
+    for (int w = 1; w < PER; ++w) {
+      const float k = __builtin_amdgcn_exp2f(sm[w][0] - top);
+      l += sm[w][1] * k;
+      o += so[w][at] * k;
+    }
   }
   store4<T>(out_row<T>(p, b, g, row, DH) + d, o * (l == 0.f ? 0.f : 1.f / l));
 }
@@ -1081,9 +1104,13 @@ void launch_dh(const TreeParams& p, const TreePlan& pl, int head_dim, hipStream_
 }
 template <typename T>
 void launch_merge(const TreeParams& p, int block_rows, int head_dim, hipStream_t s) {
-  const dim3 grid(ceil_div(p.rows, head_dim == 64 ? 16 : 8), p.batch * p.kv_heads);
-  if (head_dim == 64) attn_tree_merge<T, 64><<<grid, 256, 0, s>>>(p, block_rows);
-  else attn_tree_merge<T, 128><<<grid, 256, 0, s>>>(p, block_rows);
+  // a row over a block where it has more shares than a round trip takes and the blocks fit the chip (us, attention and merge, 8 rows a block | a row:
+  // one sequence of 8 x 4 heads, 8191 rows, one token 17.0 | 11.9, 16 21.2 | 19.6, 64 29.7 | 29.3, 3 of 7966, 4 tokens 19.4 | 16.6, 5 of 8191, 26 40.1 | 41.5)
+  const int pairs = p.batch * p.kv_heads;
+  const bool split = p.shares > 4 * pairs && (int64_t)p.rows * pairs <= 8 * compute_units();
+  const dim3 grid(split ? p.rows : ceil_div(p.rows, head_dim == 64 ? 16 : 8), pairs);
+  if (head_dim == 64) split ? attn_tree_merge<T, 64, true><<<grid, 256, 0, s>>>(p, block_rows) : attn_tree_merge<T, 64, false><<<grid, 256, 0, s>>>(p, block_rows);
+  else split ? attn_tree_merge<T, 128, true><<<grid, 256, 0, s>>>(p, block_rows) : attn_tree_merge<T, 128, false><<<grid, 256, 0, s>>>(p, block_rows);
 }
 
 }  // namespace
