@@ -1017,17 +1017,17 @@ __global__ __launch_bounds__(256) void attn_tree_merge(TreeParams p, int block_r
 // ---- how the work is cut ---------------------------------------------------------------------------------------
 // The kernel by its query rows per block, whole pairs or shares (one or two per CU), by the least estimated time: a block alone on its CU walks
 // over `alone` cache rows per us, the blocks of a full CU together over `full`, the memory gives 6.2 MB; to the largest of the three (a cubic
-// mean: they add a little) comes 1 us for every block per CU, and for shares the merge launch of 2.3 us, the partials at 4.2 MB per us and
+// mean: they add a little) comes 1 us for every block per CU, and for shares the merge launch of 3 us, the partials at 4.2 MB per us and
 // 1.4 us for every pair a share has on the average.  Of a ragged batch 0.63 of the longest cache is taken for the mean, a guess: the
 // host does not know the lengths.  The numbers were fitted so that the choices come out, not each time: 1100 drawn calls of more than 16 query
 // rows (heads of 64 and 128, 1 to 64 sequences, 3 to 64 tokens) timed at every choice; of the 200 that had no part in the fit the choice is
-// 1.3 % off the best in the geometric mean, 19 % at most.  us, whole | 256 shares | 512:
+// 1.3 % off the best in the geometric mean, 22 % at most; 210 of up to 16 rows 0.6 %, 200 in fp32 1 %.  us, whole | 256 shares | 512:
 // 7 sequences up to 4984 rows of 16 heads of 128, 5 tokens 56.8 | 39.7 | 40.4, 62 up to 137 of 8 x 4, 10 tokens, blocks of 128 rows
 // 15.8 | 27.5 | 26.5, of 32 rows 25.4 | 35.9 | 29.2, 16 up to 8191 of 8 x 4, 64 tokens, of 256 rows 195 | 124 | -, of 128 rows 167 | 145 | 133,
 // of 32 rows 181 | 221 | 181.
 struct TreePlan { int block_rows, row_blocks, shares, dealt, each; };
 struct TreeSpeed { int block_rows; float alone[2], full[2]; };      // rows per us, heads of 128: 8 bits, 16 bits
-constexpr TreeSpeed kSpeeds[] = {{16, {190.f, 200.f}, {4000.f, 430.f}}, {32, {150.f, 167.f}, {105.f, 86.f}},
+constexpr TreeSpeed kSpeeds[] = {{16, {160.f, 190.f}, {300.f, 200.f}}, {32, {150.f, 167.f}, {105.f, 86.f}},
                                  {128, {51.f, 60.f}, {54.f, 54.f}}, {256, {35.f, 40.f}, {133.f, 52.f}}};
 constexpr int MIN_CUT_ROWS = 512;         // a shorter cache is never dealt, so its calls need no workspace
 
@@ -1058,8 +1058,8 @@ TreePlan plan_tree(int batch, int q_heads, int kv_heads, int head_dim, int n, in
   for (const TreeSpeed& v : kSpeeds) {
     if (!tree_rows_ok(v.block_rows, rows, cap, f32)) continue;
     const int rb = ceil_div(rows, v.block_rows);
-    const double by = (head_dim == 128 ? 1.0 : v.block_rows == 16 ? 1.6 : v.block_rows == 32 ? 1.8 : 1.5) * (f32 ? 0.4 : 1.0);
-    const double alone = v.alone[wide] * by, full = v.full[wide] * by;
+    const double by = head_dim == 128 ? 1.0 : f32 ? 2.0 : v.block_rows == 16 ? 1.6 : v.block_rows == 32 ? 1.8 : 1.5;
+    const double alone = v.alone[wide] * by * (f32 ? 0.32 : 1.0), full = v.full[wide] * by * (f32 ? 0.2 : 1.0);
     for (int per_cu = 0; per_cu <= (v.block_rows == 256 ? 1 : 2); ++per_cu) {      // 0: whole pairs
       if (per_cu > 0 && !tree_may_deal(batch, (int64_t)batch * kv_heads, len)) break;
       const int shares = per_cu > 0 ? tree_shares((int64_t)batch * kv_heads, len, rb, per_cu) : batch * kv_heads;
@@ -1067,7 +1067,7 @@ TreePlan plan_tree(int batch, int q_heads, int kv_heads, int head_dim, int n, in
       const double a = (per_cu > 0 ? share : len) / alone, b = pairs * mean * rb / (cus * full), c = mb / 6.2;
       double us = cbrt(a * a * a + b * b * b + c * c * c) + shares * rb / cus;
       if (per_cu > 0)
-        us += 2.3 + (shares + pairs) * rb * fmin(v.block_rows, rows) * head_dim * 8e-6 / 4.2 + 1.4 * pairs / shares;
+        us += 3.0 + (shares + pairs) * rb * fmin(v.block_rows, rows) * head_dim * 8e-6 / 4.2 + 1.4 * pairs / shares;
       if (best.block_rows == 0 || us < least) {
         least = us;
         best = {v.block_rows, rb, shares, per_cu > 0, 0};
