@@ -1074,12 +1074,19 @@ TreePlan plan_tree(int batch, int q_heads, int kv_heads, int head_dim, int n, in
       }
     }
   }
-  // A short cache has fewer tiles than a block waves; where blocks have to wait for others, a wave per pair instead.  us, a block | a
-  // wave a pair, one token: 55 x 12 pairs of 64 up to 22 rows 9.0 | 4.9, 64 x 8 of 128 up to 28 8.7 | 5.7, 99 x 8 up to 82 14.0 | 10.2; time of the
-  // wave against the block's: 1 to 2 pairs a CU up to 96 rows 0.7 to 0.95, up to 256 1.0 to 1.2; more pairs up to 192 rows 0.65 to 0.95, up to 400 1.0 to 1.1.
-  // (rows in tiles of 32: 0.8 to 1.6, so not there)
+  // A short cache has fewer tiles than a block waves; where blocks have to wait for others, a wave per pair instead (of 16 query rows, also of
+  // the second 16 of up to 32).  us, a block | a wave a pair, one token: 55 x 12 pairs of 64 up to 22 rows 9.0 | 4.9, 64 x 8 of 128 up to 28 8.7 | 5.7,
+  // 99 x 8 up to 82 14.0 | 10.2; time of the wave against the block's: 1 to 2 pairs a CU up to 96 rows 0.7 to 0.95, up to 256 1.0 to 1.2; more pairs
+  // up to 192 rows 0.65 to 0.95, up to 400 1.0 to 1.1; 17 to 32 query rows up to 192 rows 0.6 to 0.9, up to 256 0.9 to 1.05 (62 x 16 up to 86, 17 tokens
+  // 30.6 | 20.3); 33 query rows and more 0.8 to 1.3, so not there
   const int64_t blocks = (int64_t)best.shares * best.row_blocks;
-  best.each = best.block_rows == 16 && !best.dealt && blocks > compute_units() && len <= (blocks > 2 * compute_units() ? 192 : 96);
+  const bool two = best.block_rows > 16 && rows <= 32 && cap >= TILE;
+  if (!best.dealt && blocks > compute_units() &&
+      (two ? len <= 192 : best.block_rows == 16 && len <= (blocks > 2 * compute_units() ? 192 : 96))) {
+    best.each = 1;
+    best.block_rows = 16;
+    best.row_blocks = ceil_div(rows, 16);
+  }
   return best;
 }
 

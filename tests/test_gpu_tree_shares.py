@@ -135,7 +135,8 @@ def test_an_infinity_reaches_those_that_see_it(n, Hq, pos, store):
 
 @pytest.mark.parametrize("store", STORES)
 @pytest.mark.parametrize("B,n,Hq,Hkv,dh,top", [
-    (50, 1, 12, 12, 64, 20), (100, 4, 12, 4, 128, 60), (65, 3, 16, 8, 64, 190), (400, 2, 2, 1, 128, 31), (33, 16, 8, 8, 128, 70), (37, 5, 21, 7, 128, 32)])
+    (50, 1, 12, 12, 64, 20), (100, 4, 12, 4, 128, 60), (65, 3, 16, 8, 64, 190), (400, 2, 2, 1, 128, 31), (33, 16, 8, 8, 128, 70), (37, 5, 21, 7, 128, 32),
+    (60, 17, 8, 8, 128, 90), (90, 8, 12, 3, 64, 170), (300, 11, 2, 1, 64, 33)])
 def test_many_short_caches(B, n, Hq, Hkv, dh, top, store):
     rng = np.random.default_rng(B + n + 2)
     check_call(rng, store, B, n, Hq, Hkv, dh, lengths(rng, B, top, "ragged"), spare=int(rng.integers(0, 3)) + 8 * (top < 31))
