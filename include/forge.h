@@ -444,7 +444,8 @@ forge_status forge_kv_read(const forge_kv_cache* cache, int layer, void* k_out, 
  * not implied).  visible: DEVICE uint64 [batch, n], or NULL: t sees the new rows 0 .. t.  A token that sees
  * nothing gets zeros; what lies in rows that a token does not see, infinities and NaN among it, does not reach it.
  * q: [batch, n, q_heads, head_dim]; out: [batch, n, q_heads * head_dim] dense, in dt.  fp32 scores, statistics and sums; for
- * bf16 the weights are rounded to bf16 for the second product.  q_heads a multiple of kv_heads.
+ * bf16 the weights are rounded to bf16 for the second product.  q_heads a multiple of kv_heads; (batch * kv_heads + 8) times
+ * the sixteens of q_heads / kv_heads * n query rows stay below 2^24.
  * The workspace size is for these lengths and every smaller max_pos. */
 size_t forge_attn_tree_workspace_bytes(const forge_kv_cache* cache, int q_heads, int n, int max_pos);
 forge_status forge_attn_tree(const forge_kv_cache* cache, int layer, const forge_heads* q, void* out,
