@@ -441,7 +441,7 @@ forge_status forge_kv_read(const forge_kv_cache* cache, int layer, void* k_out, 
 /* Attention of n new tokens per sequence (1 <= n <= 64) over layer `layer`, their rows already appended:
  *   out[b, t, h*dh : (h+1)*dh] = sum_j P[b,h,t,j] v[b, g(h), j, :],  P = softmax over the rows j that t sees of scale * q . k
  * Token t sees the cached rows j < seq_pos[b], and row seq_pos[b] + i if bit i of visible[b, t] is set (its own bit too: it is
- * not implied).  visible: DEVICE uint64 [batch, n], or NULL: t sees the new rows 0 .. t.  A token that sees
+ * not implied; bits n and above count for nothing).  visible: DEVICE uint64 [batch, n], or NULL: t sees the new rows 0 .. t.  A token that sees
  * nothing gets zeros; what lies in rows that a token does not see, infinities and NaN among it, does not reach it.
  * q: [batch, n, q_heads, head_dim]; out: [batch, n, q_heads * head_dim] dense, in dt.  fp32 scores, statistics and sums; for
  * bf16 the weights are rounded to bf16 for the second product.  q_heads a multiple of kv_heads; (batch * kv_heads + 8) times

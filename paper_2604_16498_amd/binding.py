@@ -163,13 +163,14 @@ def _dt(t: torch.Tensor) -> int:
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream():
     if _raw_stream is None:
         return C.c_void_p(torch.cuda.current_stream().cuda_stream)
     # the same handle without the Stream object around it (2.8 -> 0.2 us a call)
-    return _raw_stream(torch._C._cuda_getDevice())
+    return _raw_stream(_device())
 
 
 def _ws(t: Optional[torch.Tensor]):
@@ -458,10 +459,13 @@ def _heads(t: torch.Tensor) -> Heads:
     return Heads(t.data_ptr(), sb, st, sh)
 
 
+_INT32 = torch.int32
+
+
 def _int32(t: Optional[torch.Tensor], shape, what: str):
     if t is None:
         return None
-    if t.dtype != torch.int32 or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+    if t.dtype is not _INT32 or t.shape != shape or not t.is_cuda or not t.is_contiguous():
         raise ValueError("%s must be a contiguous int32 GPU tensor of shape %s" % (what, tuple(shape)))
     return t.data_ptr()
 
