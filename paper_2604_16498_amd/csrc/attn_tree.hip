@@ -458,7 +458,11 @@ __global__ __launch_bounds__(NW * 64, RT == 1 && sizeof(T) == 2 && (S != FORGE_K
   const int piece_row = lane / (L::ROW / 16), piece_at = lane % (L::ROW / 16) * 16;
   const int k_put = L::k_slot(piece_row) * L::STRIDE + piece_at, v_put = TILE * L::STRIDE + piece_row * L::STRIDE + piece_at;
   uint64_t marks = 0;
-  auto put_tile = [&](int behind) {        // behind: the tile's first row less the new ones' first
+  // behind: the tile's first row less the new ones' first; again: rows that the tile before had too, of a tile moved back (so that behind +
+  // TILE > 0).  Their weights are 0 here: an infinity in them would become NaN, so their V is cleared, by a loop that needs few registers;
+  // and a draft among them is not marked, the share may not hold it (this wave's own tiles lie too far apart to have marked one of them;
+  // EACH: all rows are this wave's).  fp8 has no infinities, and who sees the row of a NaN gets it either way.
+  auto put_tile = [&](int behind, int again) {
     wave_lds_sync();                       // the tile before has been read
     if (S != FORGE_KV_INT8 && behind + TILE > 0) {
 #pragma unroll
@@ -469,6 +473,11 @@ __global__ __launch_bounds__(NW * 64, RT == 1 && sizeof(T) == 2 && (S != FORGE_K
       *reinterpret_cast<u32x4*>(lds + k_put + L::k_slot(i * L::PER) * L::STRIDE) = rk[i];
 #pragma unroll
     for (int i = 0; i < L::LOADS; ++i) *reinterpret_cast<u32x4*>(lds + v_put + i * L::PER * L::STRIDE) = rv[i];
+    if (S == FORGE_KV_SAME && again > 0) {
+      if (!EACH && behind + again > 0) marks &= ~0ull << (behind + again);
+#pragma unroll 1
+      for (int o = lane * 4; o < again * L::STRIDE; o += 256) *reinterpret_cast<uint32_t*>(lds + TILE * L::STRIDE + o) = 0;
+    }
     if constexpr (SCALED) *reinterpret_cast<float*>(lds + L::SCALES + lane * 4) = rs;
     wave_lds_sync();
   };
@@ -604,7 +613,7 @@ __global__ __launch_bounds__(NW * 64, RT == 1 && sizeof(T) == 2 && (S != FORGE_K
   };
 
   for (int t = 0; t < ntile; ++t) {
-    put_tile(read_base(t) - pos);
+    put_tile(read_base(t) - pos, tile_base(t) - read_base(t));
     load_tile(t + 1, t + 1 < ntile);
     step(t);
   }
