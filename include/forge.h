@@ -382,7 +382,7 @@ typedef enum {
   FORGE_ROPE_SCALE_BANDS = 3, FORGE_ROPE_SCALE_RAMP = 4
 } forge_rope_scaling;
 
-/* HOST function: what each pair turns a position, in units of 2^-64 of a full turn (rounded), into increments
+/* HOST function: what each pair turns a position, in units of 2^-64 of a full turn (to two units), into increments
  * (HOST, rot_dim / 2 entries), and the factor of cos and sin.  In these units position * increment is exact modulo whole turns
  * for every 32-bit position: there is no large angle to reduce.  context, low and high are only looked at by BANDS and RAMP.
  * Errors: rot_dim < 2, odd or above 1024, base <= 1, by < 1, context or low <= 0, high <= low, anything not finite. */

@@ -122,24 +122,27 @@ forge_status forge_rope_increments(double base, int rot_dim, forge_rope_scaling 
   const bool banded = scaling == FORGE_ROPE_SCALE_BANDS || scaling == FORGE_ROPE_SCALE_RAMP;
   if (banded && !(std::isfinite(context) && context > 0.0 && std::isfinite(high) && low > 0.0 && high > low))
     return FORGE_ERR_INVALID_ARG;
-  const double turn = 6.283185307179586476925;
-  if (scaling == FORGE_ROPE_SCALE_BASE) base *= std::pow(by, rot_dim / (rot_dim - 2.0));
-  if (!std::isfinite(base)) return FORGE_ERR_INVALID_ARG;
-  double first = 0.0, last = 1.0;
+  // long double has 64 significant bits on the host: in 53 a fast pair's increment is off by some hundred units, a few 1e-7 of its angle at the last positions
+  typedef long double real;
+  const real turn = 6.283185307179586476925286766559L;
+  real grown = base;
+  if (scaling == FORGE_ROPE_SCALE_BASE) grown *= std::pow((real)by, rot_dim / (rot_dim - (real)2.0));
+  if (!std::isfinite((double)grown)) return FORGE_ERR_INVALID_ARG;
+  real first = 0.0, last = 1.0;
   if (scaling == FORGE_ROPE_SCALE_RAMP) {
-    auto pair = [&](double turns) { return rot_dim * std::log(context / (turns * turn)) / (2.0 * std::log(base)); };
-    first = std::fmax(0.0, std::floor(pair(high)));
-    last = std::fmin(rot_dim - 1.0, std::ceil(pair(low)));
+    auto pair = [&](real turns) { return rot_dim * std::log(context / (turns * turn)) / (2 * std::log(grown)); };
+    first = std::fmax((real)0.0, std::floor(pair(high)));
+    last = std::fmin((real)(rot_dim - 1), std::ceil(pair(low)));
   }
   for (int i = 0; i < rot_dim / 2; ++i) {
-    double theta = std::pow(base, -2.0 * i / rot_dim), g = 1.0;
+    real theta = std::pow(grown, (real)(-2 * i) / rot_dim), g = 1.0;
     if (scaling == FORGE_ROPE_SCALE_LINEAR) g = 0.0;
-    if (scaling == FORGE_ROPE_SCALE_BANDS) g = (context * theta / turn - low) / (high - low);
+    if (scaling == FORGE_ROPE_SCALE_BANDS) g = (context * theta / turn - low) / ((real)high - low);
     // (bands that coincide: a step)
-    if (scaling == FORGE_ROPE_SCALE_RAMP) g = 1.0 - (i - first) / std::fmax(1e-3, last - first);
-    g = std::fmin(1.0, std::fmax(0.0, g));
-    if (scaling != FORGE_ROPE_SCALE_NONE && scaling != FORGE_ROPE_SCALE_BASE) theta *= g + (1.0 - g) / by;
-    increments[i] = (uint64_t)std::rint(theta / turn * 18446744073709551616.0);
+    if (scaling == FORGE_ROPE_SCALE_RAMP) g = 1 - (i - first) / std::fmax((real)1e-3, last - first);
+    g = std::fmin((real)1.0, std::fmax((real)0.0, g));
+    if (scaling != FORGE_ROPE_SCALE_NONE && scaling != FORGE_ROPE_SCALE_BASE) theta *= g + (1 - g) / by;
+    increments[i] = (uint64_t)std::rint(theta / turn * 18446744073709551616.0L);
   }
   *factor = scaling == FORGE_ROPE_SCALE_RAMP ? (float)(0.1 * std::log(by) + 1.0) : 1.0f;
   return FORGE_OK;
