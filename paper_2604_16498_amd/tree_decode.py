@@ -97,6 +97,8 @@ class TreeDecoder:
         """ids [B, n]: node 0 the root, then drafts; parents[b][t] < t the node that draft t follows (of the root -1).  -> the
         model's choice after every node, [B, n]."""
         B, n = ids.shape
+        if B != self.batch or len(parents) != B:
+            raise ValueError("one tree for each of the %d sequences" % self.batch)
         if n > self.drafts or any(len(p) != n or p[0] != -1 or any(not 0 <= q < t for t, q in enumerate(p) if t) for p in parents):
             raise ValueError("each tree has one root, node 0, and at most %d nodes, parents first" % self.drafts)
         bits, depth = [[0] * n for _ in range(B)], [[0] * n for _ in range(B)]
