@@ -111,7 +111,11 @@ class TreeDecoder:
         return self._choose(self._pass(ids.contiguous(), positions, signed, max(self.held)))
 
     def commit(self, branches: Sequence[Sequence[int]], n: int) -> None:
-        """branches[b]: the accepted nodes of a tree of n, from the root down."""
+        """branches[b]: the accepted nodes of a tree of n, from the root down (none: the cache stays as it was)."""
+        if len(branches) != self.batch or not 1 <= n <= min(64, self.cap - max(self.held)):
+            raise ValueError("one branch for each of the %d sequences, of a tree that fits the cache" % self.batch)
+        if any(not -1 < t < n or (i and t <= p[i - 1]) for p in branches for i, t in enumerate(p)):
+            raise ValueError("a branch names nodes of its tree, each behind the one before")
         path = torch.tensor([list(p) + [0] * (n - len(p)) for p in branches], dtype=torch.int32, device="cuda")
         taken = torch.tensor([len(p) for p in branches], dtype=torch.int32, device="cuda")
         F.forge_kv_commit(self.cache, path, taken, self.seq_pos, max(self.held))
