@@ -4,7 +4,8 @@ loop uses them.  ``python -m paper_2604_16498_amd.tree_decode`` runs it on a sma
 A step takes, per sequence, the last token that was chosen (the root) and drafts that may follow it, as a tree.  One pass of the
 layers gives the model's choice after every node (`TreeDecoder.verify`).  Walking from the root along drafts that agree with it
 finds the accepted branch, whose cache rows are moved together (`TreeDecoder.commit`); the choice after its last node
-is the next root.  The tokens are those of one-by-one greedy decoding, several a pass where drafts agree.
+is the next root.  The tokens are those of one-by-one greedy decoding up to rounding, several a pass where drafts agree: more rows a
+pass run other kernels, which add up in another order, so two tokens whose logits are a rounding apart may change places.
 """
 from __future__ import annotations
 
