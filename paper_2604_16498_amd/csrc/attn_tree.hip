@@ -17,9 +17,12 @@
 // The rows of all (sequence, cache head) pairs are dealt evenly over the blocks in units of 128 where that is estimated to pay, whatever the lengths,
 // which only the device knows: every block finds its share from the positions.  A pair that one block holds whole is
 // finished there; of the others fp32 partials go to the workspace and a second kernel merges them in order.  No atomics.
-// Measured, 32 heads over 8 of 128: one token, 64 sequences up to 2049 rows, int8 (174 MB) 37 us, 4.7 TB/s: memory.  26 tokens, 5 up to 8217 rows, fp8
-// 32 + 6 us, 0.34 PFLOP/s; 64 tokens, 16 up to 8255, bf16 107 + 12 us, 0.8 PFLOP/s: a SIMD's matrix and vector cycles, which add up whichever
-// of its waves they come from, then the partials.  One token, 334 rows of 12 heads of 64: 5.8 us, a chain of loads.
+// Measured, 32 heads over 8 of 128: one token, 64 sequences up to 2049 rows, int8 (174 MB) 38 us, 4.6 TB/s: memory.  26 tokens, 5 up to 8217 rows, fp8
+// 38 us, 6 of them the merge, 0.29 PFLOP/s; 64 tokens, 16 up to 8255, bf16 121 us, 12 of them the merge, 0.72 PFLOP/s (the launch alone 104 to
+// 140 us by the clock that the card holds): a SIMD's matrix and vector cycles, which add up whichever of its waves they come from, then the
+// partials.  One token, 334 rows of 12 heads of 64: 5.8 us, a chain of loads.  fp32, 12 heads of 64, 8 up to 1000 rows, one token 18, 32 tokens 21 us.
+// Registers: of the kernel of 128 query rows for 16-bit heads of 128 14 are spilled (60 bytes a lane), the wide ones for 8-bit heads of 64 spill 50
+// to 117 scalar ones into vector registers.
 #include <float.h>
 #include <math.h>
 #include "tree.hpp"

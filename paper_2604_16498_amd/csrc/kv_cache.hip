@@ -1,8 +1,9 @@
 // A cache that holds its rows in 8 bits: written with the rotation, read back, and its accepted rows moved together.
 // Memory- and latency-bound; every row is touched once, in accesses of 8 and 16 bytes.  Rows of heads of 128, measured:
-//   append  8192 tokens x (16 q + 32 k, v), bf16 to fp8 (169 MB): 39 us, 4.3 TB/s, the vector ALU half busy (13 instructions an element);
-//           24 x 13 tokens x (32 q + 16 k, v) to int8 (8 MB): 5.5 us
-//   read    4 x 8191 rows x 16, int8 to bf16 (203 MB): 38 us, 5.3 TB/s
+//   append  8192 tokens x (16 q + 32 k, v), bf16 to fp8 (169 MB): 38 to 41 us, 4.1 to 4.4 TB/s, kept as they are (201 MB) 47 us, 4.3 TB/s: latency at
+//           4 waves per SIMD with two rows in flight (the vector ALU is half busy to 8 bits, 13 instructions an element);
+//           24 x 13 tokens x (32 q + 16 k, v) to int8 (7 MB): 4.6 to 5.4 us, as they are 4.3
+//   read    4 x 8191 rows x 16, int8 to bf16 (203 MB): 37 us, 5.5 TB/s
 //   commit  8 layers x 24 sequences x 16 heads, up to 26 rows: 3.8 us; 12 x 1 x 24 of 64, up to 5: 2.0, a launch
 #include "tree.hpp"
 #include "rope_rows.hpp"

@@ -5,8 +5,8 @@
 // turns and nothing else, so that neither a table by position nor fp64 is needed and cos / sin are good to 1.2e-7 at any
 // position.  A thread owns 16 elements of a token's rows that hold 8 whole pairs (two runs of 8: both halves of the pairs, or
 // neighbours) and walks over a group of heads, whose angles are the same, two rows requested while two are turned.
-// Measured: 4096 tokens x 40 heads of 128 in bf16 (84 MB) 17 us, 4.9 TB/s, where a copy of as many bytes takes 18; 3 tokens x 24 heads of
-// 64 in fp32 3.1 us, the time of a launch.  Stores that pass the caches by are faster alone (15 us) and slower with what reads the
+// Measured: 4096 tokens x 40 heads of 128 in bf16 (84 MB) 17 us, 4.9 TB/s, where a copy of as many bytes takes 18; in
+// fp32 (168 MB) 43 us, 3.9 TB/s at 3 waves per SIMD; 3 tokens x 24 heads of 64 in fp32 3.1 us, the time of a launch.  Stores that pass the caches by are faster alone (15 us) and slower with what reads the
 // rows next (32 MB and a reader 29.7 against 33.0 us), so they are ordinary ones.
 #include "tree.hpp"
 #include "rope_rows.hpp"

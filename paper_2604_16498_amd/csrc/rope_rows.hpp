@@ -87,8 +87,9 @@ struct PairTurns {
 };
 
 // Head groups (the grid's second axis): enough for 4 waves per SIMD, at most one per head; long prompts share the angles of a token
-// among the heads of a group, a few tokens are spread over all heads.  The 100 registers of these kernels let 4 or 5 waves run at
-// once.  us for 2 | 4 | 8 | 16: rotation of 4096 tokens x 40 heads of 128 19.1 | 19.9 | 21.5 | 23.5, of 8192 x 32 36.8 | 30.6 | 32.8 | 35.8; append of
+// among the heads of a group, a few tokens are spread over all heads.  As many as the registers let run, about: 92 to 110 of them, 4 or 5 waves, for
+// 16-bit rotation and 8-bit append; 80 and up to 6 for 16-bit append, 110 to 132 and 3 or 4 in fp32, where more groups were not
+// measured.  us for 2 | 4 | 8 | 16: rotation of 4096 tokens x 40 heads of 128 19.1 | 19.9 | 21.5 | 23.5, of 8192 x 32 36.8 | 30.6 | 32.8 | 35.8; append of
 // 8192 x 48 to fp8 43.7 | 40.7 | 41.8 | 43.1, of 2048 x 48 to int8 11.7 | 12.0 | 12.8 | 15.0.
 inline int row_head_groups(int64_t blocks, int heads) {
   const int64_t g = ceil_div64(4 * (int64_t)compute_units(), blocks);

@@ -16,10 +16,11 @@ constexpr int kMaxPairs = 65535;          // (sequence, cache head) pairs of one
 // The kernel by its query rows per block, whole pairs or shares (one or two per CU), by the least estimated time: a block alone on its CU walks
 // over `alone` cache rows per us, the blocks of a full CU together over `full`, the memory gives 6.2 MB; to the largest of the three (a cubic
 // mean: they add a little) comes 1 us for every block per CU, and for shares the merge launch of 3 us, the partials at 4.2 MB per us and
-// 1.4 us for every pair a share has on the average.  Of a ragged batch 0.63 of the longest cache is taken for the mean, a guess: the
-// host does not know the lengths.  The numbers were fitted so that the choices come out, not each time: 1100 drawn calls of more than 16 query
-// rows (heads of 64 and 128, 1 to 64 sequences, 3 to 64 tokens) timed at every choice; of the 200 that had no part in the fit the choice is
-// 1.3 % off the best in the geometric mean, 22 % at most; 210 of up to 16 rows 0.6 %, 200 in fp32 1 %.  us, whole | 256 shares | 512:
+// 1.4 us for every pair a share has on the average.  The host does not know a ragged batch's lengths; 0.63 of the longest cache is taken for
+// the mean, that of lengths spread evenly from a quarter to all, as in the calls that the other numbers were fitted to (1100 drawn ones of more than
+// 16 query rows, heads of 64 and 128, 1 to 64 sequences, 3 to 64 tokens, timed at every choice).  What the choice costs over the best one, in the
+// geometric mean and at most, 250 other calls of 1 to 64 tokens each: lengths like that 1.3 and 27 %, all alike 1.3 and 29 %, one long cache among
+// short ones 4.3 and 62 % (by sizes in profiles/tree_cut_choice.md).  Anything from 0.4 in its place moves these by less than a point.  us, whole | 256 shares | 512:
 // 7 sequences up to 4984 rows of 16 heads of 128, 5 tokens 56.8 | 39.7 | 40.4, 62 up to 137 of 8 x 4, 10 tokens, blocks of 128 rows
 // 15.8 | 27.5 | 26.5, of 32 rows 25.4 | 35.9 | 29.2, 16 up to 8191 of 8 x 4, 64 tokens, of 256 rows 195 | 124 | -, of 128 rows 167 | 145 | 133,
 // of 32 rows 181 | 221 | 181.
