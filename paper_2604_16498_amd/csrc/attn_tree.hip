@@ -355,7 +355,7 @@ __device__ inline void take_out(u32x4& piece, int row, int n, uint64_t& marks) {
   }
   marks |= any != 0 && row < n ? 1ull << (row & 63) : 0ull;
 }
-// those of columns d .. d + 3 that query token `tok` sees, added to its sums
+// those of columns d .. d + 3 that query token `tok` sees, added to its sums (whatever the row's weight: one that rounds to 0 is positive)
 template <typename St, int DH>
 __device__ inline void put_back(const TreeParams& p, int b, int tok, uint64_t marks, const char* vb, int pos, int d, floatx4& o) {
   for (uint64_t m = marks & bits_of(p, b, tok); m != 0; m &= m - 1) {
@@ -955,6 +955,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_tree_wide_kernel(TreeParam
   }
 }
 
+// 2^x, the weight of a share that lies -x below the largest; one that would round to 0 is the smallest positive number, so that an infinity that was
+// put back there stays one
+__device__ inline float share_weight(float x) { return fmaxf(__builtin_amdgcn_exp2f(x), __uint_as_float(1)); }
+
 // The shares of a query row in order, 4 a round trip: DH / 4 lanes a row.  Rows that one share held whole are there already.
 // SPLIT: all lanes of the block for one row, the shares in as many runs, added in their order at the end (32 shares a pair, 4 rows of 8 pairs: 8 -> 4 us).
 template <typename T, int DH, bool SPLIT>
@@ -990,14 +994,14 @@ __global__ __launch_bounds__(256) void attn_tree_merge(TreeParams p, int block_r
     float mn = mx;
 #pragma unroll
     for (int z = 0; z < 4; ++z) mn = fmaxf(mn, mz[z]);
-    const float a = __builtin_amdgcn_exp2f(mx - mn);
+    const float a = share_weight(mx - mn);
     mx = mn;
     l *= a;
     o *= a;
 #pragma unroll
     for (int z = 0; z < 4; ++z)
       if (z0 + z < to) {
-        const float w = __builtin_amdgcn_exp2f(mz[z] - mn);
+        const float w = share_weight(mz[z] - mn);
         l += lz[z] * w;
         o += oz[z] * w;
       }
@@ -1010,12 +1014,12 @@ __global__ __launch_bounds__(256) void attn_tree_merge(TreeParams p, int block_r
     float top = mx;
 #pragma unroll
     for (int w = 1; w < PER; ++w) top = fmaxf(top, sm[w][0]);
-    const float a = __builtin_amdgcn_exp2f(mx - top);
+    const float a = share_weight(mx - top);
     l *= a;
     o *= a;
 #pragma unroll
     for (int w = 1; w < PER; ++w) {
-      const float k = __builtin_amdgcn_exp2f(sm[w][0] - top);
+      const float k = share_weight(sm[w][0] - top);
       l += sm[w][1] * k;
       o += so[w][at] * k;
     }
