@@ -20,7 +20,7 @@ constexpr int kMaxPairs = 65535;          // (sequence, cache head) pairs of one
 // the mean, that of lengths spread evenly from a quarter to all, as in the calls that the other numbers were fitted to (1100 drawn ones of more than
 // 16 query rows, heads of 64 and 128, 1 to 64 sequences, 3 to 64 tokens, timed at every choice).  What the choice costs over the best one, in the
 // geometric mean and at most, 250 other calls of 1 to 64 tokens each: lengths like that 1.3 and 27 %, all alike 1.3 and 29 %, one long cache among
-// short ones 4.3 and 62 % (by sizes in profiles/tree_cut_choice.md).  Anything from 0.4 in its place moves these by less than a point.  us, whole | 256 shares | 512:
+// short ones 4.3 and 62 %.  Anything from 0.4 in its place moves these by less than a point.  us, whole | 256 shares | 512:
 // 7 sequences up to 4984 rows of 16 heads of 128, 5 tokens 56.8 | 39.7 | 40.4, 62 up to 137 of 8 x 4, 10 tokens, blocks of 128 rows
 // 15.8 | 27.5 | 26.5, of 32 rows 25.4 | 35.9 | 29.2, 16 up to 8191 of 8 x 4, 64 tokens, of 256 rows 195 | 124 | -, of 128 rows 167 | 145 | 133,
 // of 32 rows 181 | 221 | 181.
