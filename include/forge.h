@@ -469,6 +469,101 @@ forge_status forge_decoder_block_tree(const forge_block_desc* desc, const forge_
                                       void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------
+ * Many requests over one pool of cache pages.  A request's rows lie in pages of `page_rows` rows, anywhere in the pool; a table
+ * names them in order.  A step of a serving loop: forge_pages_assign gives every new token of every request (packed one request
+ * behind another) its slot, forge_paged_append writes their rows there, forge_attn_paged attends with one new token per request
+ * (a prompt: forge_attn_fused, over its own rows or over a history from forge_paged_read), forge_adapters_add adds each request's
+ * low-rank adapter to a projection.  All sizes that change from step to step lie in device memory, so one recorded graph serves them.
+ * A slot is page * page_rows + row.
+ * ------------------------------------------------------------------------------------ */
+
+/* The pool's bookkeeping, owned and initialised by the caller: free_pages the numbers of the free pages, of which *free_count
+ * count (it is a stack, the last one is taken first); table [batch, table_cols], of which request b's first
+ * ceil(length / page_rows) entries name its pages.  No page may be in two places.  (Tables that share pages can be attended over;
+ * they must not be shrunk here.)  n_pages * page_rows and table_cols * page_rows stay below 2^31.  HOST struct, device pointers. */
+typedef struct {
+  int n_pages, page_rows;       /* page_rows: a power of two, 16 .. 1024 */
+  int batch, table_cols;
+  int32_t *free_pages, *free_count, *table;     /* [n_pages], [1], [batch, table_cols] */
+} forge_page_pool;
+
+/* The requests' lengths change by change[b]: > 0 so many new tokens; < 0 as many rows fewer, at most all (a request that ended;
+ * drafts that were dropped); 0 nothing.  First the pages that are no longer needed go to the stack, by request and column, their table entries
+ * become -1; then pages are taken for the new rows.  A request is refused (its length stays) where its table has too
+ * few columns, where its tokens would pass max_tokens, or where it needs pages and those that it and the requests before it need
+ * are more than there are (requests refused for another reason need none).  So which ones are refused does not depend on timing.
+ * lengths_out[b] (may be lengths) = lengths[b] + granted[b]; granted[b]: the change that took place.
+ * Tokens, packed by request, refused ones with them: request b's are starts[b] .. starts[b + 1] - 1 ([batch + 1], at most max_tokens).  For each
+ * slots: where its row goes (-1: refused), positions: its row in its request, owners: its request.  Entries behind the last token, up to
+ * max_tokens, get -1, 0, -1.  All int32; lengths outside [0, table_cols * page_rows] are clamped; a table entry outside [0, n_pages) gives
+ * slots of -1.  max_tokens may be 0, slots, positions and owners NULL then. */
+forge_status forge_pages_assign(const forge_page_pool* pool, const int32_t* lengths, const int32_t* change, int32_t* lengths_out,
+                                int32_t* granted, int32_t* starts, int32_t* slots, int32_t* positions, int32_t* owners,
+                                int max_tokens, void* stream);
+
+/* The pages of n_layers layers.  k, v: layer l, page p, head h, row r at element
+ * l * layer_stride + p * page_stride + h * head_stride + r * head_dim (strides in elements, multiples of head_dim; layers, pages and
+ * heads must not overlap).  Types, scales and rounding as in forge_kv_cache.  HOST struct, device pointers. */
+typedef struct {
+  forge_kv_type type;
+  forge_dtype dt;               /* of the rows that go in and come out */
+  int n_layers, n_pages, page_rows, kv_heads, head_dim;     /* head_dim 64 or 128; page_rows as in forge_page_pool */
+  int64_t layer_stride, page_stride, head_stride;
+  void *k, *v;
+  float *k_scale, *v_scale;     /* NULL for FORGE_KV_SAME */
+} forge_paged_cache;
+
+/* forge_kv_append for packed tokens: k rotated (rope != NULL, then positions too) and v of token t go to slot slots[t] of layer `layer`; q
+ * (NULL: none) is rotated into q_out.  k, v, q, q_out: [token, head, head_dim] views (their batch_stride is not looked at).  A token whose slot is
+ * outside the pool is left out: no row is written for it, neither of k and v nor of q_out.  Two tokens with the same slot leave a row of
+ * unspecified content there, nowhere else. */
+forge_status forge_paged_append(const forge_paged_cache* cache, int layer, const forge_rope_desc* rope, const forge_heads* k,
+                                const forge_heads* v, const forge_heads* q, const forge_heads* q_out, int q_heads,
+                                const int32_t* slots, const int32_t* positions, int tokens, void* stream);
+
+/* The rows in slots[0 .. tokens - 1] of layer `layer`, as the values they stand for, rounded once to dt, into [token, head, head_dim] views (head-major
+ * ones, as forge_attn_fused takes them, among them; their batch_stride is not looked at).  Slots may repeat.  A token whose slot is
+ * outside the pool is left out: its rows of k_out and v_out stay as they were. */
+forge_status forge_paged_read(const forge_paged_cache* cache, int layer, const forge_heads* k_out, const forge_heads* v_out,
+                              const int32_t* slots, int tokens, void* stream);
+
+/* Attention of one new token per request over layer `layer`, its row already appended:
+ *   out[b, h*dh : (h+1)*dh] = sum_j P[b,h,j] v[b, g(h), j, :],  P = softmax over the rows j < lengths[b] of scale * q[b,h] . k[b,g(h),j]
+ * lengths: DEVICE int32 [batch], clamped to [0, max_len]; a request of length 0 (an idle place) gets zeros.  max_len: HOST, 1 ..
+ * table_cols * page_rows, sizes the launch and the workspace.  table: DEVICE int32 [batch, table_cols]; entries are clamped to
+ * [0, n_pages), so that a bad one gives a wrong result for that request, never an access outside the pool; those past a request's last
+ * row are not used.  What lies in rows behind a length, infinities and NaN among it, does not reach the output.
+ * q: [batch, head, head_dim] view (its token_stride is not looked at); out: [batch, q_heads * head_dim] dense, in dt.  fp32 scores, statistics and
+ * sums; for bf16 the weights are rounded to bf16 for the second product.  q_heads a multiple of kv_heads; (batch * kv_heads + 8) times the sixteens of
+ * q_heads / kv_heads stay below 2^24.  The workspace size serves every smaller max_len and batch too. */
+size_t forge_attn_paged_workspace_bytes(const forge_paged_cache* cache, int q_heads, int batch, int max_len);
+forge_status forge_attn_paged(const forge_paged_cache* cache, int layer, const forge_heads* q, void* out, const int32_t* lengths,
+                              const int32_t* table, int table_cols, int q_heads, int batch, int max_len, float scale,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/* Low-rank adapters beside one projection [N, K], which may be several side by side (query, key and value heads): part p has columns
+ * part_end[p - 1] (p = 0: 0) .. part_end[p] - 1 and its own A.  a: [n_adapters, n_parts * rank, K]; b: [n_adapters, N, rank]; scale: fp32
+ * [n_adapters] or NULL (1).  An adapter of a smaller rank is filled up with zeros.  HOST struct, device pointers. */
+typedef struct {
+  forge_dtype dt;
+  int n_adapters, rank;         /* rank: a multiple of 8, at most 128 */
+  int K, N;                     /* K a multiple of 8 (bf16) or 4 (fp32) */
+  int n_parts;                  /* 1 .. 4 */
+  int part_end[4];              /* rising, all but the last (= N) multiples of 16 */
+  const void *a, *b;
+  const float* scale;
+} forge_adapters;
+
+/* y[m, n] = base[m, n] + scale[i] * sum_r b[i, n, r] * (sum_k a[i, part(n) * rank + r, k] x[m, k]),  i = ids[m]
+ * x: [M, K]; base, y: [M, N] with row stride ldy (0: N); base may be y, x must not be.  ids: DEVICE int32 [M]; rows whose id is outside [0, n_adapters)
+ * get base alone (not touched where y is base).  For the output of a projection without an activation, int8 or not: y = base = that output.
+ * fp32 sums, also of the first product (bf16: as two bf16 parts in the second), one rounding to dt.  Rows of a request next to one another share the reads
+ * of its adapter.  The workspace is required where its size is not 0; the size for M serves every smaller one. */
+size_t forge_adapters_workspace_bytes(const forge_adapters* adapters, int M);
+forge_status forge_adapters_add(const forge_adapters* adapters, const void* x, const void* base, void* y, const int32_t* ids,
+                                int M, int ldy, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
  * Static buffer plan of a flat instruction list (Sec. "Phase 4: IR Analysis & Optimization").
  * HOST functions on HOST arrays; they never touch the GPU.
  * A program has n_instr instructions over registers 0..n_regs-1: instruction j writes

@@ -59,6 +59,26 @@ class KvCache(C.Structure):
     ]
 
 
+class PagePool(C.Structure):
+    _fields_ = [("n_pages", C.c_int), ("page_rows", C.c_int), ("batch", C.c_int), ("table_cols", C.c_int),
+                ("free_pages", C.c_void_p), ("free_count", C.c_void_p), ("table", C.c_void_p)]
+
+
+class PagedCache(C.Structure):
+    _fields_ = [
+        ("type", C.c_int), ("dt", C.c_int), ("n_layers", C.c_int), ("n_pages", C.c_int), ("page_rows", C.c_int),
+        ("kv_heads", C.c_int), ("head_dim", C.c_int), ("layer_stride", C.c_int64), ("page_stride", C.c_int64),
+        ("head_stride", C.c_int64), ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+    ]
+
+
+class Adapters(C.Structure):
+    _fields_ = [
+        ("dt", C.c_int), ("n_adapters", C.c_int), ("rank", C.c_int), ("K", C.c_int), ("N", C.c_int), ("n_parts", C.c_int),
+        ("part_end", C.c_int * 4), ("a", C.c_void_p), ("b", C.c_void_p), ("scale", C.c_void_p),
+    ]
+
+
 class ModelDesc(C.Structure):
     _fields_ = [
         ("n_layers", C.c_int), ("vocab", C.c_int), ("n_pos", C.c_int), ("logits_ld", C.c_int),
@@ -72,6 +92,7 @@ _lib = None
 _vp, _i, _f, _sz, _i64 = C.c_void_p, C.c_int, C.c_float, C.c_size_t, C.c_int64
 _ip, _szp = C.POINTER(C.c_int), C.POINTER(C.c_size_t)
 _d, _hp, _rp, _kvp = C.c_double, C.POINTER(Heads), C.POINTER(RopeDesc), C.POINTER(KvCache)
+_pgp, _pcp, _adp = C.POINTER(PagePool), C.POINTER(PagedCache), C.POINTER(Adapters)
 
 # name -> (restype, argtypes); the single list of what include/forge.h declares
 SIGNATURES = {
@@ -112,6 +133,13 @@ SIGNATURES = {
     "forge_kv_commit": (_i, [_kvp, _vp, _vp, _vp, _i, _i, _vp]),
     "forge_decoder_block_tree_workspace_bytes": (_sz, [C.POINTER(BlockDesc), _kvp, _i, _i]),
     "forge_decoder_block_tree": (_i, [C.POINTER(BlockDesc), _rp, _kvp, _i, _vp, _vp, _vp, _vp, _vp, _i, _i, _vp, _sz, _vp]),
+    "forge_pages_assign": (_i, [_pgp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp]),
+    "forge_paged_append": (_i, [_pcp, _i, _rp, _hp, _hp, _hp, _hp, _i, _vp, _vp, _i, _vp]),
+    "forge_paged_read": (_i, [_pcp, _i, _hp, _hp, _vp, _i, _vp]),
+    "forge_attn_paged_workspace_bytes": (_sz, [_pcp, _i, _i, _i]),
+    "forge_attn_paged": (_i, [_pcp, _i, _hp, _vp, _vp, _vp, _i, _i, _i, _i, _f, _vp, _sz, _vp]),
+    "forge_adapters_workspace_bytes": (_sz, [_adp, _i]),
+    "forge_adapters_add": (_i, [_adp, _vp, _vp, _vp, _vp, _i, _i, _vp, _sz, _vp]),
     "forge_plan_liveness": (_i, [_i, _ip, _ip, _ip, _i, _ip, _ip]),
     "forge_plan_dead_after": (_i, [_i, _ip, _i, _ip, _ip]),
     "forge_plan_linear_scan": (_i, [_i, _ip, _ip, _ip, _ip]),
@@ -615,6 +643,139 @@ def forge_decoder_block_tree(desc: BlockDesc, cache: KvCache, x_in, x_out, seq_p
                                           _visible(visible, (B, n)), n, max_pos, wp, wb, _stream()),
            "forge_decoder_block_tree")
     return x_out
+
+
+# ---------------------------------------------------------------------------------------------
+# Many requests over one pool of cache pages.
+
+
+def make_page_pool(free_pages, free_count, table, page_rows) -> PagePool:
+    """free_pages int32 [n_pages], the stack of free pages' numbers, of which free_count [1] count; table int32 [batch, cols].
+    The struct keeps them alive."""
+    if free_pages.dim() != 1 or table.dim() != 2:
+        raise ValueError("free_pages must be [n_pages], table [batch, cols]")
+    p = PagePool(free_pages.shape[0], page_rows, table.shape[0], table.shape[1], _int32(free_pages, free_pages.shape, "free_pages"),
+                 _int32(free_count, (1,), "free_count"), _int32(table, table.shape, "table"))
+    p._tensors = (free_pages, free_count, table)
+    return p
+
+
+def forge_pages_assign(pool: PagePool, lengths, change, lengths_out, granted, starts, slots=None, positions=None, owners=None):
+    """Lengths change by change[b] (int32 [batch]), pages move, and every new token gets slots, positions and owners (int32
+    [max_tokens], or all None); granted [batch]: the changes that took place; starts [batch + 1]: the tokens of every request."""
+    B = (pool.batch,)
+    T = (0,) if slots is None else (slots.shape[0],)
+    if (slots is None) != (positions is None) or (slots is None) != (owners is None):
+        raise ValueError("slots, positions and owners come together")
+    for t, what in ((lengths, "lengths"), (change, "change"), (lengths_out, "lengths_out"), (granted, "granted"), (starts, "starts")):
+        if t is None:
+            raise ValueError("%s is required" % what)
+    _check(lib().forge_pages_assign(C.byref(pool), _int32(lengths, B, "lengths"), _int32(change, B, "change"),
+                                    _int32(lengths_out, B, "lengths_out"), _int32(granted, B, "granted"),
+                                    _int32(starts, (pool.batch + 1,), "starts"), _int32(slots, T, "slots"),
+                                    _int32(positions, T, "positions"), _int32(owners, T, "owners"), T[0], _stream()),
+           "forge_pages_assign")
+
+
+def make_paged_cache(k, v, k_scale=None, v_scale=None) -> PagedCache:
+    """k, v: [pages,Hkv,rows,dh] or, of all layers, [L,pages,Hkv,rows,dh] views whose rows are dense, in bf16, fp32, int8 or
+    float8_e4m3fn; the 8-bit ones with fp32 scales of the same shape and strides without dh.  The struct keeps them alive."""
+    flat = make_kv_cache(k, v, k_scale, v_scale)          # (the same views: pages in the place of sequences)
+    return _keeping(PagedCache(flat.type, flat.dt, flat.n_layers, flat.batch, flat.cap, flat.kv_heads, flat.head_dim, flat.layer_stride,
+                               flat.batch_stride, flat.head_stride, flat.k, flat.v, flat.k_scale, flat.v_scale), flat._tensors)
+
+
+def _keeping(desc, tensors):
+    desc._tensors = tensors
+    return desc
+
+
+def _rows(t: torch.Tensor) -> Heads:
+    """A [token, head, head_dim] view, any strides, head_dim dense."""
+    st, sh, sd = t.stride()
+    if not t.is_cuda or (sd != 1 and t.shape[2] != 1):
+        raise ValueError("forge needs [token, head, head_dim] GPU tensors with a dense last axis")
+    return Heads(t.data_ptr(), 0, st, sh)
+
+
+def forge_paged_append(cache: PagedCache, k, v, slots, rope=None, positions=None, q=None, q_out=None, layer=0):
+    """k, v [T,Hkv,dh] views into the rows of slots [T], k rotated at positions [T]; q [T,Hq,dh] rotated into q_out (may be q)."""
+    T, heads, dh = k.shape
+    if heads != cache.kv_heads or dh != cache.head_dim or v.shape != k.shape:
+        raise ValueError("k and v must be [T, %d, %d]" % (cache.kv_heads, cache.head_dim))
+    if (q is None) != (q_out is None) or slots is None:
+        raise ValueError("q and q_out come together, slots always")
+    if q is None:
+        q_heads, qp, qop = 0, None, None
+        _cache_dt(cache, k, v)
+    else:
+        q_heads = q.shape[1]
+        if q.shape != (T, q_heads, dh) or q_out.shape != q.shape:
+            raise ValueError("q and q_out must be [%d, Hq, %d]" % (T, dh))
+        _cache_dt(cache, k, v, q, q_out)
+        qp, qop = C.byref(_rows(q)), C.byref(_rows(q_out))
+    _check(lib().forge_paged_append(C.byref(cache), layer, None if rope is None else C.byref(rope), C.byref(_rows(k)), C.byref(_rows(v)),
+                                    qp, qop, q_heads, _int32(slots, (T,), "slots"), _int32(positions, (T,), "positions"), T, _stream()),
+           "forge_paged_append")
+
+
+def forge_paged_read(cache: PagedCache, k_out, v_out, slots, layer=0):
+    """k_out, v_out [T,Hkv,dh] views: the rows of slots [T] as values in the cache's activation type."""
+    T, heads, dh = k_out.shape
+    if (heads, dh) != (cache.kv_heads, cache.head_dim) or v_out.shape != k_out.shape or slots is None:
+        raise ValueError("k_out and v_out must be [T, %d, %d]" % (cache.kv_heads, cache.head_dim))
+    _cache_dt(cache, k_out, v_out)
+    _check(lib().forge_paged_read(C.byref(cache), layer, C.byref(_rows(k_out)), C.byref(_rows(v_out)), _int32(slots, (T,), "slots"), T,
+                                  _stream()), "forge_paged_read")
+    return k_out, v_out
+
+
+def forge_attn_paged_workspace_bytes(cache: PagedCache, q_heads, batch, max_len) -> int:
+    return lib().forge_attn_paged_workspace_bytes(C.byref(cache), q_heads, batch, max_len)
+
+
+def forge_attn_paged(cache: PagedCache, q, out, lengths, table, max_len, scale=None, workspace=None, layer=0):
+    """q [B,Hq,dh] view; out [B,Hq*dh]; request b attends to its first lengths[b] rows (none: zeros), in the pages table[b] names."""
+    B, H, dh = q.shape
+    if dh != cache.head_dim or out.shape != (B, H * dh) or lengths is None or table.dim() != 2:
+        raise ValueError("q must be [B, Hq, %d], out [B, Hq * %d], table [B, cols]" % (cache.head_dim, cache.head_dim))
+    _cache_dt(cache, q, out)
+    view = _rows(q)
+    view.batch_stride, view.token_stride = view.token_stride, 0
+    wp, wb = _ws(workspace)
+    _check(lib().forge_attn_paged(C.byref(cache), layer, C.byref(view), _p(out), _int32(lengths, (B,), "lengths"),
+                                  _int32(table, (B, table.shape[1]), "table"), table.shape[1], H, B, max_len,
+                                  dh ** -0.5 if scale is None else scale, wp, wb, _stream()), "forge_attn_paged")
+    return out
+
+
+def make_adapters(a, b, scale=None, part_end=None) -> Adapters:
+    """a [n, parts * rank, K], b [n, N, rank], scale fp32 [n] or None; part_end: the columns at which the parts of N end (None: one).
+    The struct keeps them alive."""
+    n, N, rank = b.shape
+    ends = [N] if part_end is None else [int(e) for e in part_end]
+    if not 1 <= len(ends) <= 4 or a.shape[0] != n or a.shape[1] != len(ends) * rank or a.dtype != b.dtype:
+        raise ValueError("a must be [n, parts * rank, K] and b [n, N, rank], 1 to 4 parts")
+    if scale is not None and (scale.dtype != torch.float32 or scale.shape != (n,)):
+        raise ValueError("scale must be fp32 of shape (%d,)" % n)
+    return _keeping(Adapters(_dt(a), n, rank, a.shape[2], N, len(ends), (C.c_int * 4)(*ends), _p(a), _p(b), _p(scale)), (a, b, scale))
+
+
+def forge_adapters_workspace_bytes(adapters: Adapters, M) -> int:
+    return lib().forge_adapters_workspace_bytes(C.byref(adapters), M)
+
+
+def forge_adapters_add(adapters: Adapters, x, base, y, ids, workspace=None):
+    """y[m, :N] = base[m, :N] + the adapter ids[m] of x[m] (none where it is outside the range); y may be base, and both wider than N."""
+    M, K = x.shape
+    if K != adapters.K or base.shape != y.shape or y.shape[0] != M or ids is None:
+        raise ValueError("x must be [M, %d], base and y [M, at least %d]" % (adapters.K, adapters.N))
+    if not x.dtype == base.dtype == y.dtype or _dt(x) != adapters.dt:
+        raise ValueError("x, base, y and the adapters must agree in dtype")
+    wp, wb = _ws(workspace)
+    _check(lib().forge_adapters_add(C.byref(adapters), _p(x), _p(base), _p(y), _int32(ids, (M,), "ids"), M, y.shape[1], wp, wb, _stream()),
+           "forge_adapters_add")
+    return y
 
 
 # ---------------------------------------------------------------------------------------------

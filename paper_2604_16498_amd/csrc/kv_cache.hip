@@ -5,7 +5,7 @@
 //           24 x 13 tokens x (32 q + 16 k, v) to int8 (7 MB): 4.6 to 5.4 us, as they are 4.3
 //   read    4 x 8191 rows x 16, int8 to bf16 (203 MB): 37 us, 5.5 TB/s
 //   commit  8 layers x 24 sequences x 16 heads, up to 26 rows: 3.8 us; 12 x 1 x 24 of 64, up to 5: 2.0, a launch
-#include "tree.hpp"
+#include "paged.hpp"
 #include "rope_rows.hpp"
 
 namespace forge {
@@ -36,7 +36,8 @@ __device__ inline float divide(float x, float scale, float r) {
 // A thread per 16 elements of a token's rows and group of heads (blockIdx.y), as the rotation alone; the q heads come first, then
 // those of k and v.  The row's maximum is taken over the bits of |x|: as integers they order like the values, infinities and
 // NaN above all.
-template <typename T, forge_kv_type S, int DH, bool HALF>
+// PAGED: tokens go to slots of their own, one whose slot is outside the pool is left out.
+template <typename T, forge_kv_type S, int DH, bool HALF, bool PAGED>
 __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs p, uint32_t total) {
   constexpr int ITEMS = DH / 16;
   const uint32_t gid = blockIdx.x * 256u + threadIdx.x;
@@ -54,7 +55,9 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs p, uint32_t t
     const int hh = h < nq ? h : h < nq + p.kv_heads ? h - nq : h - nq - p.kv_heads;
     return reinterpret_cast<const T*>(x.p) + b * x.bs + i * x.ts + hh * x.hs;
   };
+  bool live = true;                      // (the same for all lanes of a row)
   auto finish = [&](int h, float (&a)[8], float (&c)[8]) {
+    if (PAGED && !live) return;
     const bool is_v = h >= nq + p.kv_heads;
     if (!is_v) w.turn(a, c);                                  // (rows of v are split as those of k: any 16 elements of the row do)
     if (h < nq) {
@@ -103,10 +106,18 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs p, uint32_t t
     }
   };
   walk_heads<T>(h0, h1, w.e0, w.e1, source, [&] {
-    const int row = first_row(p.seq_pos, b, p.max_pos) + i;
-    at_row = b * p.c.bs + (int64_t)row * DH;
-    at_scale = at_row / DH;
-    w.at(t, p.positions != nullptr ? p.positions[tok] : row);
+    if constexpr (PAGED) {
+      const int slot = p.slots[tok];
+      live = (uint32_t)slot < (uint32_t)p.n_slots;
+      at_row = (slot >> p.shift) * p.c.bs + (int64_t)(slot & ((1 << p.shift) - 1)) * DH;
+      at_scale = at_row / DH;
+      w.at(t, p.positions != nullptr ? p.positions[tok] : 0);       // (none: no rotation)
+    } else {
+      const int row = first_row(p.seq_pos, b, p.max_pos) + i;
+      at_row = b * p.c.bs + (int64_t)row * DH;
+      at_scale = at_row / DH;
+      w.at(t, p.positions != nullptr ? p.positions[tok] : row);
+    }
   }, finish);
 }
 
@@ -132,6 +143,32 @@ __global__ __launch_bounds__(256) void kv_read_kernel(CacheView c, T* k_out, T* 
     for (int j = 0; j < 8; ++j) x[j] *= scale;
   }
   Vec8<T>::store((is_v ? v_out : k_out) + ((int64_t)b * kv_heads + h) * n * DH + at * 8, x);
+}
+
+// Rows of any slots: a thread per 8 elements of a token's row; grid (tokens in blocks, heads of k and v)
+template <typename T, forge_kv_type S, int DH>
+__global__ __launch_bounds__(256) void paged_read_kernel(PagedRows p) {
+  const int h = blockIdx.y >> 1;
+  const bool is_v = blockIdx.y & 1;
+  const uint32_t gid = blockIdx.x * 256u + threadIdx.x, tok = gid / (DH / 8), d = gid % (DH / 8) * 8;
+  if (tok >= (uint32_t)p.tokens) return;
+  const int slot = p.slots[tok], shift = p.cache.shift;
+  if ((uint32_t)slot >= (uint32_t)p.cache.n_pages << shift) return;
+  const CacheView& c = p.cache.c;
+  const int64_t e = (slot >> shift) * c.bs + h * c.hs + (int64_t)(slot & ((1 << shift) - 1)) * DH + d;
+  float x[8];
+  if constexpr (S == FORGE_KV_SAME) {
+    Vec8<T>::load(reinterpret_cast<const T*>(is_v ? c.v : c.k) + e, x);
+  } else {
+    const u32x2 w = *reinterpret_cast<const u32x2*>((is_v ? c.v : c.k) + e);
+    const float scale = (is_v ? c.vs : c.ks)[e / DH];
+    Codes<S>::unpack(w[0], x);
+    Codes<S>::unpack(w[1], x + 4);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] *= scale;
+  }
+  const Heads& y = is_v ? p.v : p.k;
+  Vec8<T>::store(reinterpret_cast<T*>(y.p) + tok * y.ts + h * y.hs + d, x);
 }
 
 // A wave per (layer, sequence, head, k or v) walks over the accepted rows in rising order, ROWS of them at a time.  In place: a
@@ -164,8 +201,13 @@ __global__ __launch_bounds__(64) void kv_commit_kernel(CacheView c, int64_t laye
 template <typename T, forge_kv_type S>
 void append_dh(const AppendArgs& a, const dim3& grid, uint32_t total, hipStream_t s) {
   auto go = [&](auto kernel) { kernel<<<grid, 256, 0, s>>>(a, total); };
-  if (a.head_dim == 64) a.t.half ? go(kv_append_kernel<T, S, 64, true>) : go(kv_append_kernel<T, S, 64, false>);
-  else a.t.half ? go(kv_append_kernel<T, S, 128, true>) : go(kv_append_kernel<T, S, 128, false>);
+  if (a.slots != nullptr) {
+    if (a.head_dim == 64) a.t.half ? go(kv_append_kernel<T, S, 64, true, true>) : go(kv_append_kernel<T, S, 64, false, true>);
+    else a.t.half ? go(kv_append_kernel<T, S, 128, true, true>) : go(kv_append_kernel<T, S, 128, false, true>);
+    return;
+  }
+  if (a.head_dim == 64) a.t.half ? go(kv_append_kernel<T, S, 64, true, false>) : go(kv_append_kernel<T, S, 64, false, false>);
+  else a.t.half ? go(kv_append_kernel<T, S, 128, true, false>) : go(kv_append_kernel<T, S, 128, false, false>);
 }
 
 template <typename T, forge_kv_type S>
@@ -174,6 +216,13 @@ void read_dh(const CacheView& c, int batch, int kv_heads, int head_dim, void* k_
   const dim3 grid((unsigned)ceil_div64((int64_t)n * (head_dim / 8), 256), 2 * kv_heads, batch);
   if (head_dim == 64) kv_read_kernel<T, S, 64><<<grid, 256, 0, s>>>(c, (T*)k_out, (T*)v_out, kv_heads, seq_pos, n, max_pos);
   else kv_read_kernel<T, S, 128><<<grid, 256, 0, s>>>(c, (T*)k_out, (T*)v_out, kv_heads, seq_pos, n, max_pos);
+}
+
+template <typename T, forge_kv_type S>
+void paged_read_dh(const PagedRows& a, hipStream_t s) {
+  const dim3 grid((unsigned)ceil_div64((int64_t)a.tokens * (a.head_dim / 8), 256), 2 * a.kv_heads);
+  if (a.head_dim == 64) paged_read_kernel<T, S, 64><<<grid, 256, 0, s>>>(a);
+  else paged_read_kernel<T, S, 128><<<grid, 256, 0, s>>>(a);
 }
 
 }  // namespace
@@ -196,6 +245,14 @@ forge_status launch_kv_read(const CacheView& c, forge_kv_type type, forge_dtype 
   else if (type == FORGE_KV_SAME) read_dh<bf16, FORGE_KV_SAME>(c, batch, kv_heads, head_dim, k_out, v_out, seq_pos, n, max_pos, s);
   else if (type == FORGE_KV_INT8) read_dh<bf16, FORGE_KV_INT8>(c, batch, kv_heads, head_dim, k_out, v_out, seq_pos, n, max_pos, s);
   else read_dh<bf16, FORGE_KV_FP8>(c, batch, kv_heads, head_dim, k_out, v_out, seq_pos, n, max_pos, s);
+  return launch_status();
+}
+
+forge_status launch_paged_read(const PagedRows& a, hipStream_t s) {
+  if (a.dt == FORGE_F32) paged_read_dh<float, FORGE_KV_SAME>(a, s);
+  else if (a.type == FORGE_KV_SAME) paged_read_dh<bf16, FORGE_KV_SAME>(a, s);
+  else if (a.type == FORGE_KV_INT8) paged_read_dh<bf16, FORGE_KV_INT8>(a, s);
+  else paged_read_dh<bf16, FORGE_KV_FP8>(a, s);
   return launch_status();
 }
 

@@ -35,6 +35,9 @@ struct AppendArgs {
   const int* positions;
   forge_kv_type type;
   forge_dtype dt;
+  // a paged cache (batch 1, c.bs the stride of a page): the row of token t is row slots[t] % (1 << shift) of page slots[t] >> shift
+  const int* slots;      // NULL: none
+  int n_slots, shift;
 };
 
 struct TreeArgs {
