@@ -11,7 +11,6 @@ namespace forge {
 namespace {
 
 constexpr int JT = 4;          // 16-wide tiles of the inner index a block works on
-constexpr int COLS = 256;      // columns of y per block, 64 a wave
 
 // Operands of 16 rows x 64 bytes: lane l has 16 bytes of row l % 16 at 16 (l / 16)
 template <typename T> struct Mma;
@@ -38,295 +37,527 @@ struct Rows {
     const int lane = threadIdx.x & 63;
     id = lane < rows && m0 + lane < p.M ? p.ids[m0 + lane] : -1;
     if ((uint32_t)id >= (uint32_t)p.n_adapters) id = -1;
-    bool first = id >= 0;
-    for (int j = 0; j < rows; ++j) first = first && !(j < lane && __builtin_amdgcn_readlane(id, j) == id);
-    leaders = __ballot(first);
+    uint64_t todo = __ballot(id >= 0);
+    leaders = 0;
+    while (todo != 0) {                  // (an adapter a turn)
+      const int l = __ffsll((unsigned long long)todo) - 1;
+      leaders |= 1ull << l;
+      todo &= ~__ballot(id == __builtin_amdgcn_readlane(id, l));
+    }
   }
 };
 
-struct Cut { int tiles, splits, chunks, lanes; };
+struct Cut { int tiles, splits, chunks, lanes, groups; };      // groups: of 64 columns, a block of the second launch
 
-// t of 16 RT rows and 64 inner columns over one range of K, shared out among the waves 128 bytes of a row at a time
-template <typename T, int RT>
-__global__ __launch_bounds__(256, RT == 1 ? 4 : 2) void adapters_inner_kernel(AdapterArgs p, Cut cut) {
-  typedef Mma<T> M;
-  constexpr int UNIT = 2 * M::STEP;
-  __shared__ __attribute__((aligned(16))) floatx4 red[4][RT][JT][64];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, kg = lane >> 4;
-  const int inner = p.parts * p.rank;
-  const int64_t m0 = (int64_t)blockIdx.x * (16 * RT);
-  const int split = blockIdx.y / cut.chunks, j0 = blockIdx.y % cut.chunks * (16 * JT);
-  const Rows rows(p, m0, 16 * RT);
-  const int units = ceil_div(p.K, UNIT);
-  const int u0 = (int)((int64_t)units * split / cut.splits), u1 = (int)((int64_t)units * (split + 1) / cut.splits);
-  const T* xr[RT];
+// 16 bytes of each of N rows at unit u of the range's n; a unit that is not there asks for one line (the loads stay, so that their number is known
+// and a wait is for no more than what it needs)
+template <typename T, int N>
+__device__ inline void load_unit(u32x4 (&r)[N], const T* const (&src)[N], const T* some, int u, int n, int k, int K, int at16) {
+  const bool in = u < n && k + at16 < K;
 #pragma unroll
-  for (int i = 0; i < RT; ++i) {
-    const int64_t m = m0 + 16 * i + c;
-    xr[i] = reinterpret_cast<const T*>(p.x) + (m < p.M ? m : p.M - 1) * p.K + kg * (16 / (int)sizeof(T));
+  for (int i = 0; i < N; ++i) r[i] = *reinterpret_cast<const u32x4*>(in ? src[i] + k : some);
+}
+// ... and into LDS, 0 past the end of K
+template <int N, int APART>
+__device__ inline void store_unit(char* to, const u32x4 (&r)[N], bool in) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4*>(to + i * APART) = in ? r[i] : u32x4{0, 0, 0, 0};
+}
+
+// t of 16 rows and 64 inner columns over one range of K, whose units of 128 bytes a row are shared out among 4 waves.  A unit of x and of the adapter comes
+// in 1 KB pieces of 8 whole lines into registers, two units ahead, and goes through LDS of its wave alone: read as operands from memory, 16 bytes of 64
+// rows a load, each lane would be a line lookup.
+template <typename T>
+__global__ __launch_bounds__(256, 2) void adapters_inner_kernel(AdapterArgs p, Cut cut) {
+  typedef Mma<T> M;
+  constexpr int PER = 16 / sizeof(T), UNIT = 8 * PER, ROW = 144, WAVES = 4;       // (rows 16 bytes apart in the banks)
+  __shared__ __attribute__((aligned(16))) char lds[WAVES][(16 + 16 * JT) * ROW];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, kg = lane >> 4;
+  const int inner = p.parts * p.rank, line = lane >> 3, at16 = (lane & 7) * PER;
+  const int64_t m0 = (int64_t)blockIdx.x * 16;
+  const int split = blockIdx.y / cut.chunks, j0 = blockIdx.y % cut.chunks * (16 * JT);
+  const int tiles = min(JT, ceil_div(inner - j0, 16));                   // of the inner index that there are here
+  const int units = ceil_div(p.K, UNIT), part = split * WAVES + wave, parts = cut.splits * WAVES;
+  const int u0 = (int)((int64_t)units * part / parts), n = (int)((int64_t)units * (part + 1) / parts) - u0;
+  const T* const some = reinterpret_cast<const T*>(p.x);
+  const T* xs[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int64_t m = m0 + 8 * i + line;
+    xs[i] = some + (m < p.M ? m : p.M - 1) * p.K + at16;
   }
+  u32x4 xf[2][2], af[2][2 * JT];                                         // two units in flight
+  auto load_x = [&](int u, u32x4 (&r)[2]) { load_unit<T>(r, xs, some, u, n, (u0 + u) * UNIT, p.K, at16); };
+  load_x(0, xf[0]);
+  load_x(1, xf[1]);
+  const Rows rows(p, m0, 16);
+  char* const patch = lds[wave];
+  uint64_t left = rows.leaders;
+  bool again = false;
+  for (int s = 0; left != 0; ++s, left &= left - 1) {
+    if (s % cut.lanes != (int)blockIdx.z) continue;
+    const int id = __builtin_amdgcn_readlane(rows.id, __ffsll((unsigned long long)left) - 1);
+    const T* as[2 * JT];
+#pragma unroll
+    for (int i = 0; i < 2 * JT; ++i)
+      as[i] = reinterpret_cast<const T*>(p.a) + ((int64_t)id * inner + min(j0 + 8 * i + line, inner - 1)) * p.K + at16;
+    auto load_a = [&](int u, u32x4 (&r)[2 * JT]) { load_unit<T>(r, as, some, u, n, (u0 + u) * UNIT, p.K, at16); };
+    floatx4 acc[JT];
+#pragma unroll
+    for (int j = 0; j < JT; ++j) acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    if (again) {
+      load_x(0, xf[0]);
+      load_x(1, xf[1]);
+    }
+    again = true;
+    load_a(0, af[0]);
+    load_a(1, af[1]);
+    auto step = [&](int u, u32x4 (&x)[2], u32x4 (&a)[2 * JT]) {
+      wave_lds_sync();
+      char* const to = patch + line * ROW + (lane & 7) * 16;
+      const bool in = (u0 + u) * UNIT + at16 < p.K;
+      store_unit<2, 8 * ROW>(to, x, in);
+      store_unit<2 * JT, 8 * ROW>(to + 16 * ROW, a, in);
+      wave_lds_sync();
+      load_x(u + 2, x);
+      load_a(u + 2, a);
+      const char* const from = patch + c * ROW + kg * 16;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(from + h * 64);
+#pragma unroll
+        for (int j = 0; j < JT; ++j)
+          if (j < tiles) acc[j] = M::go(*reinterpret_cast<const u32x4*>(from + (16 + 16 * j) * ROW + h * 64), x, acc[j]);
+      }
+    };
+    for (int u = 0; u < n; u += 2) {
+      step(u, xf[0], af[0]);
+      if (u + 1 < n) step(u + 1, xf[1], af[1]);
+    }
+    // ---- the waves' sums in order: 4 inner indices of a row a lane
+    wave_lds_sync();
+#pragma unroll
+    for (int j = 0; j < JT; ++j) *reinterpret_cast<floatx4*>(patch + j * 1024 + lane * 16) = acc[j];
+    lds_barrier();
+    floatx4 t = *reinterpret_cast<const floatx4*>(lds[0] + wave * 1024 + lane * 16);
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) t += *reinterpret_cast<const floatx4*>(lds[w] + wave * 1024 + lane * 16);
+    const int at = j0 + 16 * wave + 4 * kg, mine = __shfl(rows.id, c, 64);
+    if (mine == id && at < inner)
+      *reinterpret_cast<floatx4*>(reinterpret_cast<float*>(p.workspace) + ((int64_t)split * p.M + m0 + c) * inner + at) = t;
+    lds_barrier();
+  }
+}
+
+// The same for many rows, of which 64 next to one another mostly share an adapter: a block's waves take 16 rows each and share the adapter's units through
+// two buffers of LDS.
+template <typename T>
+__global__ __launch_bounds__(256, 2) void adapters_inner_many_kernel(AdapterArgs p, Cut cut) {
+  typedef Mma<T> M;
+  constexpr int PER = 16 / sizeof(T), UNIT = 8 * PER, ROW = 144, AHEAD = 4;
+  __shared__ __attribute__((aligned(16))) char lds[2][128 * ROW];          // rows of x, then of the adapter
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, kg = lane >> 4;
+  const int inner = p.parts * p.rank, line = tid >> 3, at16 = (tid & 7) * PER;
+  const int64_t m0 = (int64_t)blockIdx.x * 64;
+  const int split = blockIdx.y / cut.chunks, j0 = blockIdx.y % cut.chunks * (16 * JT);
+  const int tiles = min(JT, ceil_div(inner - j0, 16));
+  const int units = ceil_div(p.K, UNIT);
+  const int u0 = (int)((int64_t)units * split / cut.splits), n = (int)((int64_t)units * (split + 1) / cut.splits) - u0;
+  const T* const some = reinterpret_cast<const T*>(p.x);
+  const T* xs[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int64_t m = m0 + 32 * i + line;
+    xs[i] = some + (m < p.M ? m : p.M - 1) * p.K + at16;
+  }
+  u32x4 xf[AHEAD][2], af[AHEAD][2];
+  auto load_x = [&](int u, u32x4 (&r)[2]) { load_unit<T>(r, xs, some, u, n, (u0 + u) * UNIT, p.K, at16); };
+  bool again = blockIdx.z > 0;           // x not requested yet: few tiles have a second adapter
+  if (!again) {
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) load_x(a, xf[a]);
+  }
+  const Rows rows(p, m0, 64);
   uint64_t left = rows.leaders;
   for (int s = 0; left != 0; ++s, left &= left - 1) {
     if (s % cut.lanes != (int)blockIdx.z) continue;
     const int id = __builtin_amdgcn_readlane(rows.id, __ffsll((unsigned long long)left) - 1);
-    const T* ar[JT];
+    const T* as[2];
 #pragma unroll
-    for (int j = 0; j < JT; ++j) {
-      const int at = j0 + 16 * j + c;
-      ar[j] = reinterpret_cast<const T*>(p.a) + ((int64_t)id * inner + (at < inner ? at : inner - 1)) * p.K + kg * (16 / (int)sizeof(T));
+    for (int i = 0; i < 2; ++i)
+      as[i] = reinterpret_cast<const T*>(p.a) + ((int64_t)id * inner + min(j0 + 32 * i + line, inner - 1)) * p.K + at16;
+    auto load_a = [&](int u, u32x4 (&r)[2]) { load_unit<T>(r, as, some, u, n, (u0 + u) * UNIT, p.K, at16); };
+    if (again) {
+#pragma unroll
+      for (int a = 0; a < AHEAD; ++a) load_x(a, xf[a]);
     }
-    floatx4 acc[RT][JT];
+    again = true;
 #pragma unroll
-    for (int i = 0; i < RT; ++i)
+    for (int a = 0; a < AHEAD; ++a) load_a(a, af[a]);
+    floatx4 acc[JT];
 #pragma unroll
-      for (int j = 0; j < JT; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    u32x4 xf[2][RT][2], af[2][JT][2];
-    auto load = [&](int u, int buf) {
+    for (int j = 0; j < JT; ++j) acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    auto step = [&](int u, u32x4 (&x)[2], u32x4 (&a)[2]) {
+      char* const buf = lds[u & 1];
+      const bool in = (u0 + u) * UNIT + at16 < p.K;
+      char* const to = buf + line * ROW + (tid & 7) * 16;
+      store_unit<2, 32 * ROW>(to, x, in);
+      store_unit<2, 32 * ROW>(to + 64 * ROW, a, in);
+      load_x(u + AHEAD, x);
+      load_a(u + AHEAD, a);
+      lds_barrier();                     // (the other buffer's readers are past it)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int k = u * UNIT + h * M::STEP;
-        const bool in = k + kg * (16 / (int)sizeof(T)) < p.K;
-        const u32x4 zero = {0, 0, 0, 0};
-#pragma unroll
-        for (int i = 0; i < RT; ++i) xf[buf][i][h] = in ? *reinterpret_cast<const u32x4*>(xr[i] + k) : zero;
+        const u32x4 x = *reinterpret_cast<const u32x4*>(buf + (16 * wave + c) * ROW + h * 64 + kg * 16);
 #pragma unroll
         for (int j = 0; j < JT; ++j)
-          if (j0 + 16 * j < inner) af[buf][j][h] = in ? *reinterpret_cast<const u32x4*>(ar[j] + k) : zero;
+          if (j < tiles) acc[j] = M::go(*reinterpret_cast<const u32x4*>(buf + (64 + 16 * j + c) * ROW + h * 64 + kg * 16), x, acc[j]);
       }
     };
-    auto multiply = [&](int buf) {
+    for (int u = 0; u < n; u += AHEAD) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int j = 0; j < JT; ++j)
-          if (j0 + 16 * j < inner)
-#pragma unroll
-            for (int i = 0; i < RT; ++i) acc[i][j] = M::go(af[buf][j][h], xf[buf][i][h], acc[i][j]);
-    };
-    int u = u0 + wave;
-    if (u < u1) load(u, 0);
-    for (; u < u1; u += 8) {
-      if (u + 4 < u1) load(u + 4, 1);
-      multiply(0);
-      if (u + 8 < u1) load(u + 8, 0);
-      if (u + 4 < u1) multiply(1);
+      for (int a = 0; a < AHEAD; ++a)
+        if (u + a < n) step(u + a, xf[a], af[a]);
     }
+    lds_barrier();                       // before the next adapter's first unit
+    const int row = 16 * wave + c, mine = __shfl(rows.id, row, 64);
+    float* to = reinterpret_cast<float*>(p.workspace) + ((int64_t)split * p.M + m0 + row) * inner;
 #pragma unroll
-    for (int i = 0; i < RT; ++i)
-#pragma unroll
-      for (int j = 0; j < JT; ++j) red[wave][i][j][lane] = acc[i][j];
-    lds_barrier();
-    const int at = j0 + 16 * wave + 4 * kg;                    // a wave adds up one tile: 4 inner indices of a row a lane
-#pragma unroll
-    for (int i = 0; i < RT; ++i) {
-      const floatx4 t = red[0][i][wave][lane] + red[1][i][wave][lane] + red[2][i][wave][lane] + red[3][i][wave][lane];
-      const int mine = __shfl(rows.id, 16 * i + c, 64);
-      if (mine == id && at < inner)
-        *reinterpret_cast<floatx4*>(reinterpret_cast<float*>(p.workspace) + ((int64_t)split * p.M + m0 + 16 * i + c) * inner + at) = t;
+    for (int j = 0; j < JT; ++j) {
+      const int at = j0 + 16 * j + 4 * kg;
+      if (mine == id && at < inner) *reinterpret_cast<floatx4*>(to + at) = acc[j];
     }
-    lds_barrier();
   }
 }
 
-// 16 consecutive elements of a row as fp32
-template <typename T>
-__device__ inline void load16(const T* p, float (&v)[16]) {
-  float a[8], b[8];
-  Vec8<T>::load(p, a);
-  Vec8<T>::load(p + 8, b);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) { v[i] = a[i]; v[8 + i] = b[i]; }
-}
-template <typename T>
-__device__ inline void store16(T* p, const float (&v)[16]) {
-  float a[8], b[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) { a[i] = v[i]; b[i] = v[8 + i]; }
-  Vec8<T>::store(p, a);
-  Vec8<T>::store(p + 8, b);
-}
+// 4 elements of a row of y
+template <typename T> struct Four;
+template <> struct Four<float> {
+  typedef u32x4 type;
+  static __device__ inline u32x4 added(u32x4 w, const floatx4& v) { return __builtin_bit_cast(u32x4, __builtin_bit_cast(floatx4, w) + v); }
+};
+template <> struct Four<bf16> {
+  typedef u32x2 type;
+  static __device__ inline u32x2 added(u32x2 w, const floatx4& v) {
+    return u32x2{pack_bf2(bf_lo(w[0]) + v[0], bf_hi(w[0]) + v[1]), pack_bf2(bf_lo(w[1]) + v[2], bf_hi(w[1]) + v[3])};
+  }
+};
 
-// y of 16 RT rows and 64 columns a wave.  The rows of b in tile i of its 64 columns are 16 (r / 4) + 4 i + r % 4, so that a lane ends up with 16
-// consecutive columns of its row.  bf16: t as the sum of two bf16 numbers, 16 bits of it, in two products.  NS: steps of the rank.
-template <typename T, int RT, int NS>
-__global__ __launch_bounds__(256, 2) void adapters_outer_kernel(AdapterArgs p, Cut cut) {
-  typedef Mma<T> M;
-  constexpr bool F32 = sizeof(T) == 4;
-  constexpr int PER = 16 / sizeof(T);      // elements of a lane's 16 bytes
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, kg = lane >> 4;
-  const int inner = p.parts * p.rank;
-  const int chunks = ceil_div(p.N, COLS);
-  const int64_t m0 = (int64_t)(blockIdx.x / chunks) * (16 * RT);
-  const int n0 = blockIdx.x % chunks * COLS + 64 * wave;
-  if (n0 >= p.N) return;
-  const Rows rows(p, m0, 16 * RT);
-  const bool whole = n0 + 16 * kg + 16 <= p.N && p.ldy % 8 == 0;       // this lane's 16 columns, at addresses for wide accesses
-  auto finish = [&](int i, const float (&add)[16], const float (&old)[16]) {
-    const int64_t at = (m0 + 16 * i + c) * p.ldy + n0 + 16 * kg;
-    T* y = reinterpret_cast<T*>(p.y) + at;
-    if (whole) {
-      float v[16];
+// t of `rows` rows of one part, added up over the ranges: fours of a row's inner indices, thread q % THREADS has four q
+template <typename T, int NS, int ROWS>
+struct Inner {
+  static constexpr bool F32 = sizeof(T) == 4;
+  static constexpr int QUADS = NS * (Mma<T>::STEP / 4), ALL = ROWS * QUADS, EACH = (ALL + 255) / 256;
+  static constexpr int ROW = NS * 64 + 16, PLANE = ROWS * ROW, BYTES = (F32 ? 1 : 2) * PLANE;      // in LDS (rows apart in the banks)
+  floatx4 t[EACH];
+  __device__ inline void load(const AdapterArgs& p, int splits, int64_t m0, int rows_left, int part) {
+    const int inner = p.parts * p.rank;
+    const int64_t plane = (int64_t)p.M * inner;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) v[e] = old[e] + add[e];
-      store16<T>(y, v);
-    } else {
-      const T* b = reinterpret_cast<const T*>(p.base) + at;
+    for (int i = 0; i < EACH; ++i) {
+      const int q = (int)threadIdx.x + 256 * i, row = min(q / QUADS, rows_left - 1), r = q % QUADS;
+      t[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+      if (q >= ALL || r >= p.rank / 4) continue;
+      const float* from = reinterpret_cast<const float*>(p.workspace) + (m0 + row) * inner + part * p.rank + 4 * r;
+      for (int z = 0; z < splits; z += 8) {
+        floatx4 v[8];
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (n0 + 16 * kg + e < p.N) y[e] = from_f32<T>(to_f32<T>(b[e]) + add[e]);
-    }
-  };
-  auto old_of = [&](int i, float (&old)[16]) {
-    if (whole) load16<T>(reinterpret_cast<const T*>(p.base) + (m0 + 16 * i + c) * p.ldy + n0 + 16 * kg, old);
-  };
-  if (blockIdx.y == 0 && p.y != p.base) {                      // rows without an adapter
+        for (int k = 0; k < 8; ++k)
+          if (z + k < splits) v[k] = *reinterpret_cast<const floatx4*>(from + (z + k) * plane);
 #pragma unroll
-    for (int i = 0; i < RT; ++i) {
-      const int mine = __shfl(rows.id, 16 * i + c, 64);
-      if (mine >= 0 || m0 + 16 * i + c >= p.M) continue;
-      const float none[16] = {};
-      float old[16];
-      old_of(i, old);
-      finish(i, none, old);
+        for (int k = 0; k < 8; ++k)
+          if (z + k < splits) t[i] += v[k];
+      }
     }
   }
+  // bf16: as the sum of two bf16 numbers, 16 bits of it
+  template <typename Scale>
+  __device__ inline void store(char* lds, Scale scale) const {
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int q = (int)threadIdx.x + 256 * i;
+      if (q >= ALL) continue;
+      const floatx4 v = t[i] * scale(q / QUADS);
+      char* to = lds + q / QUADS * ROW + q % QUADS * (int)(4 * sizeof(T));
+      if constexpr (F32) *reinterpret_cast<floatx4*>(to) = v;
+      else {
+        const u32x2 hi = {pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3])};
+        *reinterpret_cast<u32x2*>(to) = hi;
+        *reinterpret_cast<u32x2*>(to + PLANE) = u32x2{pack_bf2(v[0] - bf_lo(hi[0]), v[1] - bf_hi(hi[0])), pack_bf2(v[2] - bf_lo(hi[1]), v[3] - bf_hi(hi[1]))};
+      }
+    }
+  }
+};
+
+// Column c of product j is column 4 c + j of a wave's 64, so that a lane ends up with 4 columns of four rows and a wave's accesses to base and y are
+// whole lines: rows n0 + 4 c + j of b, 16 bytes of a step at 16 (l / 16).
+template <typename T, int NS>
+__device__ inline void load_b(u32x4 (&bf)[4][NS], const AdapterArgs& p, int id, int n0) {
+  const int c = threadIdx.x & 15, kg = threadIdx.x >> 4 & 3;
+  constexpr int PER = 16 / sizeof(T), STEP = Mma<T>::STEP;
+  const T* const bm = reinterpret_cast<const T*>(p.b) + (int64_t)id * p.N * p.rank;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const T* b = bm + (int64_t)min(n0 + 4 * c + j, p.N - 1) * p.rank;
+#pragma unroll
+    for (int st = 0; st < NS; ++st) {
+      const int r = st * STEP + kg * PER;
+      bf[j][st] = *reinterpret_cast<const u32x4*>(b + (r < p.rank ? r : 0));
+    }
+  }
+}
+// (inner indices past the rank: t is 0 there, and an infinity must not meet it)
+template <typename T, int NS>
+__device__ inline void trim_b(u32x4 (&bf)[4][NS], int rank) {
+  const int kg = threadIdx.x >> 4 & 3;
+  constexpr int PER = 16 / sizeof(T), STEP = Mma<T>::STEP;
+  if (rank == NS * STEP) return;
+#pragma unroll
+  for (int st = NS / 2; st < NS; ++st)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) bf[j][st][e] = st * STEP + kg * PER < rank ? bf[j][st][e] : 0u;
+}
+template <typename T, int NS, int ROWS>
+__device__ inline void products(floatx4 (&acc)[4], const u32x4 (&bf)[4][NS], const char* lds, int tile) {
+  typedef Inner<T, NS, ROWS> I;
+  const int c = threadIdx.x & 15, kg = threadIdx.x >> 4 & 3;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int st = 0; st < NS; ++st) {
+    const char* from = lds + (16 * tile + c) * I::ROW + st * 64 + kg * 16;
+#pragma unroll
+    for (int h = 0; h < (I::F32 ? 1 : 2); ++h) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(from + h * I::PLANE);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j] = Mma<T>::go(x, bf[j][st], acc[j]);
+    }
+  }
+}
+
+// y of 16 rows from m0 on and columns b0 .. b1 - 1, 64 a wave at a time; of the rows' adapters every `lanes`-th from `lane0` on.  t0: t of the part that
+// b0 belongs to, requested before the adapters are known.
+template <typename T, int NS>
+__device__ inline void outer_rows(const AdapterArgs& p, const Cut& cut, int lanes, int lane0, int64_t m0, int b0, int b1, char* tl) {
+  typedef typename Four<T>::type F;
+  typedef Inner<T, NS, 16> I;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, kg = lane >> 4;
+  const int rows_left = (int)min((int64_t)16, p.M - m0);
   int part0 = 0, part1 = 0;                                    // the parts that these columns belong to
-  const int last = min(n0 + 63, p.N - 1);
-  while (n0 >= p.part_end[part0]) ++part0;
-  while (last >= p.part_end[part1]) ++part1;
-  int my_part = part0;                                         // of this lane's 16 columns
-  while (my_part < part1 && n0 + 16 * kg >= p.part_end[my_part]) ++my_part;
-
+  while (b0 >= p.part_end[part0]) ++part0;
+  while (b1 - 1 >= p.part_end[part1]) ++part1;
+  I t;
+  t.load(p, cut.splits, m0, rows_left, part0);
+  int have = part0;
+  const Rows rows(p, m0, 16);
+  const T* const base = reinterpret_cast<const T*>(p.base) + m0 * p.ldy;
+  T* const y = reinterpret_cast<T*>(p.y) + m0 * p.ldy;
+  const bool wide = p.ldy % 4 == 0;        // rows at addresses for wide accesses
+  if (lane0 == 0 && p.y != p.base) {                           // rows without an adapter
+    const uint32_t none = (uint32_t)__ballot(rows.id < 0) & ((1u << rows_left) - 1);
+    for (int n = b0 + 4 * lane; n < b1; n += 256) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int64_t at = (int64_t)(4 * i + wave) * p.ldy + n;
+        if (!(none >> (4 * i + wave) & 1)) continue;
+        if (wide && n + 4 <= b1) *reinterpret_cast<F*>(y + at) = *reinterpret_cast<const F*>(base + at);
+        else
+          for (int j = 0; j < 4 && n + j < b1; ++j) y[at + j] = base[at + j];
+      }
+    }
+  }
   uint64_t left = rows.leaders;
   for (int s = 0; left != 0; ++s, left &= left - 1) {
-    if (s % cut.lanes != (int)blockIdx.y) continue;
+    if (s % lanes != lane0) continue;
     const int id = __builtin_amdgcn_readlane(rows.id, __ffsll((unsigned long long)left) - 1);
     const float scale = p.scale != nullptr ? p.scale[id] : 1.f;
-    u32x4 bf[4][NS];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int n = min(n0 + 16 * (c >> 2) + 4 * i + (c & 3), p.N - 1);
-      const T* b = reinterpret_cast<const T*>(p.b) + ((int64_t)id * p.N + n) * p.rank;
-#pragma unroll
-      for (int st = 0; st < NS; ++st) {
-        const int r = st * M::STEP + kg * PER;
-        bf[i][st] = r < p.rank ? *reinterpret_cast<const u32x4*>(b + r) : u32x4{0, 0, 0, 0};
-      }
-    }
-#pragma unroll 1
+    const uint32_t here = (uint32_t)__ballot(rows.id == id);   // this adapter's rows; t of the others is multiplied along
     for (int part = part0; part <= part1; ++part) {
+      const int first = max(b0, part == 0 ? 0 : p.part_end[part - 1]) + 64 * wave, end = min(b1, p.part_end[part]);
+      u32x4 bf[4][NS];
+      F old[4];
+      auto request = [&](int n0) {
+        load_b<T, NS>(bf, p, id, n0);
+        if (!wide || n0 + 4 * c + 4 > end) return;
 #pragma unroll
-      for (int i = 0; i < RT; ++i) {
-        const int mine = __shfl(rows.id, 16 * i + c, 64);
-        const bool here = mine == id && part == my_part;
-        if (__ballot(mine == id) == 0) continue;
-        float old[16];
-        if (here) old_of(i, old);
-        const int64_t m = m0 + 16 * i + c;
-        const float* t0 = reinterpret_cast<const float*>(p.workspace) + (mine == id ? m : m0 + __ffsll((unsigned long long)left) - 1) * inner + part * p.rank;
+        for (int e = 0; e < 4; ++e)
+          if ((here >> e & 0x1111) != 0)                       // (one of rows e, 4 + e, 8 + e, 12 + e)
+            old[e] = *reinterpret_cast<const F*>(base + (int64_t)min(4 * kg + e, rows_left - 1) * p.ldy + n0 + 4 * c);
+      };
+      if (first < end) request(first);
+      if (part != have) t.load(p, cut.splits, m0, rows_left, have = part);
+      t.store(tl, [&](int) { return scale; });
+      lds_barrier();
+      for (int n0 = first; n0 < end; n0 += 256) {
+        if (n0 != first) request(n0);
+        trim_b<T, NS>(bf, p.rank);
         floatx4 acc[4];
+        products<T, NS, 16>(acc, bf, tl, 0);
+        const int n = n0 + 4 * c;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
-        float t[NS][PER];
+        for (int e = 0; e < 4; ++e) {
+          if ((here >> e & 0x1111) == 0) continue;
+          if (!(here >> (4 * kg + e) & 1)) continue;
+          const floatx4 v = {acc[0][e], acc[1][e], acc[2][e], acc[3][e]};
+          const int64_t at = (int64_t)(4 * kg + e) * p.ldy + n;
+          if (wide && n + 4 <= end) *reinterpret_cast<F*>(y + at) = Four<T>::added(old[e], v);
+          else {
 #pragma unroll
-        for (int st = 0; st < NS; ++st)
-#pragma unroll
-          for (int e = 0; e < PER; ++e) t[st][e] = 0.f;
-        for (int z = 0; z < cut.splits; ++z) {
-          const float* tz = t0 + (int64_t)z * p.M * inner;
-#pragma unroll
-          for (int st = 0; st < NS; ++st) {
-            const int r = st * M::STEP + kg * PER;
-            if (r < p.rank)
-#pragma unroll
-              for (int e = 0; e < PER; e += 4) {
-                const floatx4 v = *reinterpret_cast<const floatx4*>(tz + r + e);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) t[st][e + q] += v[q];
-              }
+            for (int j = 0; j < 4; ++j)
+              if (n + j < end) y[at + j] = from_f32<T>(to_f32<T>(base[at + j]) + v[j]);
           }
-        }
-#pragma unroll
-        for (int st = 0; st < NS; ++st) {
-          u32x4 hi, lo;
-          if constexpr (F32) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) hi[e] = __float_as_uint(t[st][e] * scale);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float a = t[st][2 * e] * scale, b = t[st][2 * e + 1] * scale;
-              hi[e] = pack_bf2(a, b);
-              lo[e] = pack_bf2(a - bf_lo(hi[e]), b - bf_hi(hi[e]));
-            }
-          }
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            acc[j] = M::go(bf[j][st], hi, acc[j]);
-            if constexpr (!F32) acc[j] = M::go(bf[j][st], lo, acc[j]);
-          }
-        }
-        if (here) {
-          float add[16];
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) add[4 * j + e] = acc[j][e];
-          finish(i, add, old);
         }
       }
+      lds_barrier();
     }
   }
 }
+template <typename T, int NS>
+__global__ __launch_bounds__(256, 2) void adapters_outer_kernel(AdapterArgs p, Cut cut) {
+  __shared__ __attribute__((aligned(16))) char tl[Inner<T, NS, 16>::BYTES];
+  const int cols = 64 * cut.groups, chunks = ceil_div(p.N, cols);
+  const int b0 = blockIdx.x % chunks * cols;
+  outer_rows<T, NS>(p, cut, cut.lanes, blockIdx.y, (int64_t)(blockIdx.x / chunks) * 16, b0, min(b0 + cols, p.N), tl);
+}
 
-// Blocks of one tile until two rounds of the chip are full of tiles; K in ranges of 4 units (one a wave) at least
-Cut cut_of(int M, int K, int inner, forge_dtype dt, int rt) {
-  const int cus = compute_units(), units = ceil_div(K, dt == FORGE_BF16 ? 64 : 32);
+// Many rows: 64 of them and 256 columns of one part, 64 a wave.  Most share an adapter: base, b and t are requested at once and no row is tested (beside memory,
+// instructions bound these blocks), and a row's accesses are one offset a lane from scalar addresses.  Where they do not, one adapter after another.
+template <typename T, int NS>
+__global__ __launch_bounds__(256, 2) void adapters_outer_many_kernel(AdapterArgs p, Cut cut) {
+  typedef typename Four<T>::type F;
+  typedef Inner<T, NS, 64> I;
+  __shared__ __attribute__((aligned(16))) char tl[I::BYTES];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, kg = lane >> 4;
+  const int chunks = ceil_div(p.N, 256);
+  const int turn = blockIdx.x / 8;         // of the XCDs: each works on whole rows
+  const int64_t m0 = (int64_t)(turn / chunks * 8 + blockIdx.x % 8) * 64;
+  if (m0 >= p.M) return;
+  const int b0 = turn % chunks * 256, b1 = min(b0 + 256, p.N);
+  int part = 0;
+  while (b0 >= p.part_end[part]) ++part;
+  if (m0 + 64 > p.M || b1 - b0 != 256 || b1 > p.part_end[part] || p.ldy % 4 != 0) {
+#pragma unroll 1
+    for (int i = 0; i < 4 && m0 + 16 * i < p.M; ++i) outer_rows<T, NS>(p, cut, 1, 0, m0 + 16 * i, b0, b1, tl);
+    return;
+  }
+  const Rows rows(p, m0, 64);
+  const uint64_t none = __ballot(rows.id < 0);
+  if (none == ~0ull && p.y == p.base) return;
+  const int n0 = b0 + 64 * wave;
+  const int64_t row = p.ldy * (int64_t)sizeof(T);
+  const uint32_t at = 4 * kg * (uint32_t)row + 4 * c * (uint32_t)sizeof(T);      // (ldy is at most 2^24)
+  const char* const base = reinterpret_cast<const char*>(p.base) + m0 * row + n0 * (int64_t)sizeof(T);
+  char* const y = reinterpret_cast<char*>(p.y) + m0 * row + n0 * (int64_t)sizeof(T);
+  int id = __builtin_amdgcn_readlane(rows.id, rows.leaders != 0 ? __ffsll((unsigned long long)rows.leaders) - 1 : 0);
+  u32x4 bf[4][NS];
+  if (rows.leaders != 0) load_b<T, NS>(bf, p, id, n0);
+  F old[4][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) old[i][e] = *reinterpret_cast<const F*>(base + (16 * i + e) * row + at);
+  if (none != 0 && p.y != p.base) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (none >> (16 * i + 4 * kg + e) & 1) *reinterpret_cast<F*>(y + (16 * i + e) * row + at) = old[i][e];
+  }
+  if (rows.leaders == 0) return;
+  {
+    I t;
+    t.load(p, cut.splits, m0, 64, part);
+    t.store(tl, [&](int r) {
+      const int whose = __shfl(rows.id, r, 64);
+      return p.scale != nullptr ? p.scale[max(whose, 0)] : 1.f;
+    });
+  }
+  lds_barrier();
+  for (uint64_t left = rows.leaders;;) {
+    const uint64_t here = __ballot(rows.id == id);
+    trim_b<T, NS>(bf, p.rank);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      __builtin_amdgcn_sched_barrier(0);   // (a tile's operands at a time, or they fill the registers)
+      floatx4 acc[4];
+      products<T, NS, 64>(acc, bf, tl, i);
+      if (here == ~0ull) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          *reinterpret_cast<F*>(y + (16 * i + e) * row + at) = Four<T>::added(old[i][e], floatx4{acc[0][e], acc[1][e], acc[2][e], acc[3][e]});
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (here >> (16 * i + 4 * kg + e) & 1)
+            *reinterpret_cast<F*>(y + (16 * i + e) * row + at) = Four<T>::added(old[i][e], floatx4{acc[0][e], acc[1][e], acc[2][e], acc[3][e]});
+      }
+    }
+    left &= left - 1;
+    if (left == 0) break;
+    id = __builtin_amdgcn_readlane(rows.id, __ffsll((unsigned long long)left) - 1);
+    load_b<T, NS>(bf, p, id, n0);
+  }
+}
+
+// From here on the blocks take 64 rows: most of them share an adapter with their neighbours
+constexpr int MANY = 1024;
+
+// K in ranges until the blocks fill the chip, of two units a wave (a block, of many rows: four) at least
+Cut cut_of(int M, int K, int inner, forge_dtype dt) {
+  const bool many = M >= MANY;
+  const int units = ceil_div(K, dt == FORGE_BF16 ? 64 : 32), least = many ? 4 : 8;
   Cut c;
-  c.tiles = ceil_div(M, 16 * rt);
+  c.tiles = ceil_div(M, many ? 64 : 16);
   c.chunks = ceil_div(inner, 16 * JT);
   const int64_t blocks = (int64_t)c.tiles * c.chunks;
-  const int want = (int)ceil_div64(2 * cus, blocks), most = units < 4 ? 1 : units / 4;
+  const int want = (int)ceil_div64((many ? 1 : 2) * compute_units(), blocks), most = units < least ? 1 : units / least;
   c.splits = want < 1 ? 1 : want < most ? want : most;
-  c.lanes = 1;
+  c.lanes = c.groups = 1;
   return c;
 }
-int tiles_per_block(int M) { return M >= 1024 ? 4 : 1; }
 
-template <typename T, int RT>
-forge_status launch_rt(const AdapterArgs& a, hipStream_t s) {
-  const int cus = compute_units(), inner = a.parts * a.rank;
-  Cut c = cut_of(a.M, a.K, inner, a.dt, RT);
-  auto lanes = [&](int64_t blocks) {                           // a tile of 16 rows has at most 16 adapters
-    const int64_t l = ceil_div64(8 * cus, blocks);
-    const int most = RT > 1 ? 1 : a.M < 16 ? a.M : 16;
-    return (int)(l < 1 ? 1 : l < most ? l : most);
-  };
-  c.lanes = lanes((int64_t)c.tiles * c.chunks * c.splits);
-  adapters_inner_kernel<T, RT><<<dim3(c.tiles, c.chunks * c.splits, c.lanes), 256, 0, s>>>(a, c);
-  if (hipGetLastError() != hipSuccess) return FORGE_ERR_HIP;
-  const int64_t blocks = (int64_t)c.tiles * ceil_div(a.N, COLS);
-  c.lanes = lanes(blocks);
-  const dim3 grid((unsigned)blocks, c.lanes);
-  const int steps = ceil_div(a.rank, Mma<T>::STEP);
-  if (steps == 1) adapters_outer_kernel<T, RT, 1><<<grid, 256, 0, s>>>(a, c);
-  else if (steps == 2) adapters_outer_kernel<T, RT, 2><<<grid, 256, 0, s>>>(a, c);
-  else if (steps <= 4) adapters_outer_kernel<T, RT, 4><<<grid, 256, 0, s>>>(a, c);
-  else adapters_outer_kernel<T, RT, 8><<<grid, 256, 0, s>>>(a, c);
-  return launch_status();
+template <typename T, int NS>
+void launch_outer(const AdapterArgs& a, const Cut& c, const dim3& grid, hipStream_t s) {
+  if (a.M >= MANY) adapters_outer_many_kernel<T, NS><<<grid, 256, 0, s>>>(a, c);
+  else adapters_outer_kernel<T, NS><<<grid, 256, 0, s>>>(a, c);
 }
 template <typename T>
 forge_status launch(const AdapterArgs& a, hipStream_t s) {
-  return tiles_per_block(a.M) == 4 ? launch_rt<T, 4>(a, s) : launch_rt<T, 1>(a, s);
+  const int cus = compute_units(), inner = a.parts * a.rank;
+  const bool many = a.M >= MANY;
+  Cut c = cut_of(a.M, a.K, inner, a.dt);
+  auto lanes = [&](int64_t blocks) {                           // a tile of 16 rows has at most 16 adapters
+    const int64_t l = ceil_div64(8 * cus, blocks);
+    const int most = many ? 1 : a.M < 16 ? a.M : 16;
+    return (int)(l < 1 ? 1 : l < most ? l : most);
+  };
+  c.lanes = many ? 4 : lanes((int64_t)c.tiles * c.chunks * c.splits);
+  const dim3 grid(c.tiles, c.chunks * c.splits, c.lanes);
+  if (many) adapters_inner_many_kernel<T><<<grid, 256, 0, s>>>(a, c);
+  else adapters_inner_kernel<T><<<grid, 256, 0, s>>>(a, c);
+  if (hipGetLastError() != hipSuccess) return FORGE_ERR_HIP;
+  c.groups = many || a.N <= 256 ? 4 : 8;
+  const int64_t blocks = (int64_t)(many ? ceil_div(c.tiles, 8) * 8 : c.tiles) * ceil_div(a.N, 64 * c.groups);
+  c.lanes = lanes(blocks);
+  const dim3 outer((unsigned)blocks, c.lanes);
+  const int steps = ceil_div(a.rank, Mma<T>::STEP);
+  if (steps == 1) launch_outer<T, 1>(a, c, outer, s);
+  else if (steps == 2) launch_outer<T, 2>(a, c, outer, s);
+  else if (steps <= 4) launch_outer<T, 4>(a, c, outer, s);
+  else if constexpr (sizeof(T) == 4) launch_outer<T, 8>(a, c, outer, s);
+  return launch_status();
 }
 
 }  // namespace
 
-// Room for any smaller M too: of m rows in `tiles` tiles the planes are at most units / 4, and at most 2 cus / (tiles chunks) + 1, times m rows
+// Room for any smaller M too: of m rows in `tiles` tiles the ranges are at most units / 4 (8: fewer rows), and at most 2 cus / (tiles chunks) + 1; times m
+// rows, of which a tile has at most 16 (64, but then half as many blocks are asked for)
 size_t adapters_workspace_bytes(int M, int N, int K, int rank, int parts, forge_dtype dt) {
-  const int inner = parts * rank, rt = tiles_per_block(M), units = ceil_div(K, dt == FORGE_BF16 ? 64 : 32);
-  const int64_t most = (int64_t)(units < 4 ? 1 : units / 4) * M;
-  const int64_t full = ceil_div(2 * compute_units() * 16 * rt, ceil_div(inner, 16 * JT)) + (int64_t)M;
+  const int inner = parts * rank, units = ceil_div(K, dt == FORGE_BF16 ? 64 : 32), least = M >= MANY ? 4 : 8;
+  const int64_t most = (int64_t)(units < least ? 1 : units / least) * M;
+  const int64_t full = ceil_div((M >= MANY ? 64 : 32) * compute_units(), ceil_div(inner, 16 * JT)) + (int64_t)M;
   return (size_t)(most < full ? most : full) * inner * sizeof(float);
 }
 
