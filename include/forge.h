@@ -480,7 +480,8 @@ forge_status forge_decoder_block_tree(const forge_block_desc* desc, const forge_
 /* The pool's bookkeeping, owned and initialised by the caller: free_pages the numbers of the free pages, of which *free_count
  * count (it is a stack, the last one is taken first); table [batch, table_cols], of which request b's first
  * ceil(length / page_rows) entries name its pages.  No page may be in two places.  (Tables that share pages can be attended over;
- * they must not be shrunk here.)  n_pages * page_rows and table_cols * page_rows stay below 2^31.  HOST struct, device pointers. */
+ * they must not be shrunk here.)  n_pages * page_rows and table_cols * page_rows stay below 2^31, n_pages
+ * and table_cols at most 2^25.  HOST struct, device pointers. */
 typedef struct {
   int n_pages, page_rows;       /* page_rows: a power of two, 16 .. 1024 */
   int batch, table_cols;

@@ -259,13 +259,14 @@ struct Inner {
       t[i] = floatx4{0.f, 0.f, 0.f, 0.f};
       if (q >= ALL || r >= p.rank / 4) continue;
       const float* from = reinterpret_cast<const float*>(p.workspace) + (m0 + row) * inner + part * p.rank + 4 * r;
-      for (int z = 0; z < splits; z += 8) {
-        floatx4 v[8];
+      constexpr int AT_ONCE = EACH > 2 ? 4 : 8;
+      for (int z = 0; z < splits; z += AT_ONCE) {
+        floatx4 v[AT_ONCE];
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
+        for (int k = 0; k < AT_ONCE; ++k)
           if (z + k < splits) v[k] = *reinterpret_cast<const floatx4*>(from + (z + k) * plane);
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
+        for (int k = 0; k < AT_ONCE; ++k)
           if (z + k < splits) t[i] += v[k];
       }
     }

@@ -11,6 +11,7 @@ namespace {
 // (a slot is a 32-bit number)
 bool page_rows_ok(int rows) { return rows >= 16 && rows <= 1024 && (rows & (rows - 1)) == 0; }
 bool fits_32_bits(int pages, int rows) { return (int64_t)pages * rows < ((int64_t)1 << 31); }
+constexpr int kMaxPages = 1 << 25;      // of a pool, of a table's row: 64 requests' sums then stay in 32 bits
 int shift_of(int rows) { return __builtin_ctz((unsigned)rows); }
 
 forge_status check_pages(const forge_paged_cache* c) {
@@ -94,7 +95,8 @@ forge_status forge_pages_assign(const forge_page_pool* pool, const int32_t* leng
   if (max_tokens > 0 && (slots == positions || slots == owners || positions == owners)) return FORGE_ERR_INVALID_ARG;
   for (const void* q : {slots, positions, owners})
     if (max_tokens > 0 && (q == lengths || q == change)) return FORGE_ERR_INVALID_ARG;
-  if (!page_rows_ok(pool->page_rows) || pool->batch > kMaxGridDim || max_tokens > kMaxRows ||
+  if (!page_rows_ok(pool->page_rows) || pool->batch > kMaxGridDim || max_tokens > kMaxRows || pool->n_pages > kMaxPages ||
+      pool->table_cols > kMaxPages ||
       !fits_32_bits(pool->n_pages, pool->page_rows) || !fits_32_bits(pool->table_cols, pool->page_rows))
     return FORGE_ERR_UNSUPPORTED;
   const PagesArgs a = {pool->n_pages, shift_of(pool->page_rows), pool->batch, pool->table_cols, max_tokens, pool->free_pages,
