@@ -660,21 +660,26 @@ def make_page_pool(free_pages, free_count, table, page_rows) -> PagePool:
     return p
 
 
+def _vector(t: torch.Tensor, n: int, what: str):
+    if t.dtype is not _INT32 or t.numel() != n or not t.is_cuda or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous int32 GPU tensor of %d entries" % (what, n))
+    return t.data_ptr()
+
+
 def forge_pages_assign(pool: PagePool, lengths, change, lengths_out, granted, starts, slots=None, positions=None, owners=None):
     """Lengths change by change[b] (int32 [batch]), pages move, and every new token gets slots, positions and owners (int32
     [max_tokens], or all None); granted [batch]: the changes that took place; starts [batch + 1]: the tokens of every request."""
-    B = (pool.batch,)
-    T = (0,) if slots is None else (slots.shape[0],)
-    if (slots is None) != (positions is None) or (slots is None) != (owners is None):
-        raise ValueError("slots, positions and owners come together")
-    for t, what in ((lengths, "lengths"), (change, "change"), (lengths_out, "lengths_out"), (granted, "granted"), (starts, "starts")):
-        if t is None:
-            raise ValueError("%s is required" % what)
-    _check(lib().forge_pages_assign(C.byref(pool), _int32(lengths, B, "lengths"), _int32(change, B, "change"),
-                                    _int32(lengths_out, B, "lengths_out"), _int32(granted, B, "granted"),
-                                    _int32(starts, (pool.batch + 1,), "starts"), _int32(slots, T, "slots"),
-                                    _int32(positions, T, "positions"), _int32(owners, T, "owners"), T[0], _stream()),
-           "forge_pages_assign")
+    B = pool.batch
+    if slots is None:
+        if positions is not None or owners is not None:
+            raise ValueError("slots, positions and owners come together")
+        T, sp, pp, op = 0, None, None, None
+    else:
+        T = slots.numel()
+        sp, pp, op = _vector(slots, T, "slots"), _vector(positions, T, "positions"), _vector(owners, T, "owners")
+    _check(lib().forge_pages_assign(C.byref(pool), _vector(lengths, B, "lengths"), _vector(change, B, "change"),
+                                    _vector(lengths_out, B, "lengths_out"), _vector(granted, B, "granted"),
+                                    _vector(starts, B + 1, "starts"), sp, pp, op, T, _stream()), "forge_pages_assign")
 
 
 def make_paged_cache(k, v, k_scale=None, v_scale=None) -> PagedCache:
@@ -715,8 +720,8 @@ def forge_paged_append(cache: PagedCache, k, v, slots, rope=None, positions=None
         _cache_dt(cache, k, v, q, q_out)
         qp, qop = C.byref(_rows(q)), C.byref(_rows(q_out))
     _check(lib().forge_paged_append(C.byref(cache), layer, None if rope is None else C.byref(rope), C.byref(_rows(k)), C.byref(_rows(v)),
-                                    qp, qop, q_heads, _int32(slots, (T,), "slots"), _int32(positions, (T,), "positions"), T, _stream()),
-           "forge_paged_append")
+                                    qp, qop, q_heads, _vector(slots, T, "slots"), None if positions is None else _vector(positions, T, "positions"), T,
+                                    _stream()), "forge_paged_append")
 
 
 def forge_paged_read(cache: PagedCache, k_out, v_out, slots, layer=0):
@@ -725,7 +730,7 @@ def forge_paged_read(cache: PagedCache, k_out, v_out, slots, layer=0):
     if (heads, dh) != (cache.kv_heads, cache.head_dim) or v_out.shape != k_out.shape or slots is None:
         raise ValueError("k_out and v_out must be [T, %d, %d]" % (cache.kv_heads, cache.head_dim))
     _cache_dt(cache, k_out, v_out)
-    _check(lib().forge_paged_read(C.byref(cache), layer, C.byref(_rows(k_out)), C.byref(_rows(v_out)), _int32(slots, (T,), "slots"), T,
+    _check(lib().forge_paged_read(C.byref(cache), layer, C.byref(_rows(k_out)), C.byref(_rows(v_out)), _vector(slots, T, "slots"), T,
                                   _stream()), "forge_paged_read")
     return k_out, v_out
 
@@ -743,7 +748,7 @@ def forge_attn_paged(cache: PagedCache, q, out, lengths, table, max_len, scale=N
     view = _rows(q)
     view.batch_stride, view.token_stride = view.token_stride, 0
     wp, wb = _ws(workspace)
-    _check(lib().forge_attn_paged(C.byref(cache), layer, C.byref(view), _p(out), _int32(lengths, (B,), "lengths"),
+    _check(lib().forge_attn_paged(C.byref(cache), layer, C.byref(view), _p(out), _vector(lengths, B, "lengths"),
                                   _int32(table, (B, table.shape[1]), "table"), table.shape[1], H, B, max_len,
                                   dh ** -0.5 if scale is None else scale, wp, wb, _stream()), "forge_attn_paged")
     return out
@@ -773,7 +778,7 @@ def forge_adapters_add(adapters: Adapters, x, base, y, ids, workspace=None):
     if not x.dtype == base.dtype == y.dtype or _dt(x) != adapters.dt:
         raise ValueError("x, base, y and the adapters must agree in dtype")
     wp, wb = _ws(workspace)
-    _check(lib().forge_adapters_add(C.byref(adapters), _p(x), _p(base), _p(y), _int32(ids, (M,), "ids"), M, y.shape[1], wp, wb, _stream()),
+    _check(lib().forge_adapters_add(C.byref(adapters), _p(x), _p(base), _p(y), _vector(ids, M, "ids"), M, y.shape[1], wp, wb, _stream()),
            "forge_adapters_add")
     return y
 

@@ -4,6 +4,8 @@
 //   s_j = scale q . k_j,  m = max s_j,  l = sum exp(s_j - m),  o = sum exp(s_j - m) v_j / l
 // A block of 4 waves takes the 16 query heads (or fewer) of a cache head as the columns of one matrix operand, and its waves take the 32-row tiles of
 // its range of rows in turn; the tile layouts, the products and the dealing of rows over blocks are those of the attention of drafted trees.
+// Up to 8 query heads a cache head: the 16 columns hold each twice, and the second takes what the weights of the first lose in bf16, so that they count with
+// 16 bits, for no further product (from 9 heads on they are rounded to bf16, 2^-9 each, as there).
 // What is its own is where a tile lies: in two halves of 16 rows, each inside a page, whose numbers a wave keeps in a
 // register, an entry a lane, for its next 32 tiles; a half's address is then scalar arithmetic.
 #include "cache_tiles.hpp"
@@ -61,6 +63,9 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 && (S != FORGE_KV_SAME || D
   Share<PagedParams> share;
   if (!share.start(p, EACH ? NW : 1, EACH ? wave : 0)) return;
   const int c = lane & 15, kg = lane >> 4;
+  const bool twice = !F32 && p.rows <= 8;
+  const int column = twice ? c & 7 : c;                        // the query head of this lane, counted in its block
+  const float rest = twice && c >= 8 ? 1.f : 0.f;
   char* const lds = patch[wave];
   const int in_page = (1 << p.shift) - 1;
 
@@ -101,7 +106,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 && (S != FORGE_KV_SAME || D
     head = g * p.c.hs;
     begin = from;
     load_pages(b, 0);
-    const int row = share.rb * 16 + c;
+    const int row = share.rb * 16 + column;
     const T* qr = reinterpret_cast<const T*>(p.q.p) + b * p.q.bs + (g * p.group + (row < p.rows ? row : 0)) * p.q.hs;
 #pragma unroll
     for (int j = 0; j < NQ; ++j) {
@@ -218,7 +223,10 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 && (S != FORGE_KV_SAME || D
     } else {
       u32x4 w;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = pack_bf2(s[2 * e], s[2 * e + 1]);
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t hi = pack_bf2(s[2 * e], s[2 * e + 1]);
+        w[e] = pack_bf2(__builtin_fmaf(bf_lo(hi), -rest, s[2 * e]), __builtin_fmaf(bf_hi(hi), -rest, s[2 * e + 1]));
+      }
       const bf16x8 pf = __builtin_bit_cast(bf16x8, w);
 #pragma unroll
       for (int m = 0; m < NM; ++m)
@@ -248,7 +256,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 && (S != FORGE_KV_SAME || D
   else lds_barrier();
   for (int idx = EACH ? lane : tid; idx < 16 * (DH / 4); idx += SIDE * 64) {
     const int r = idx / (DH / 4), d = idx % (DH / 4) * 4, row = share.rb * 16 + r;
-    if (row >= p.rows) continue;
+    if (row >= p.rows) continue;           // (so r < 8 where heads are there twice)
     const int w0 = EACH ? wave : 0;
     float mn = sml[w0][r][0];
 #pragma unroll
@@ -258,7 +266,13 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 && (S != FORGE_KV_SAME || D
 #pragma unroll
     for (int w = w0; w < w0 + SIDE; ++w) {
       const float a = __builtin_amdgcn_exp2f(sml[w][r][0] - mn);
-      o += *reinterpret_cast<const floatx4*>(patch[w] + r * (PAD * 4) + d * 4) * a;
+      floatx4 x = *reinterpret_cast<const floatx4*>(patch[w] + r * (PAD * 4) + d * 4);
+      if (twice) {                         // (where a row has an infinity, the first part says which)
+        const floatx4 y = *reinterpret_cast<const floatx4*>(patch[w] + (r + 8) * (PAD * 4) + d * 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] += fabsf(x[i]) < INFINITY ? y[i] : 0.f;
+      }
+      o += x * a;
       lt += sml[w][r][1] * a;
     }
     if (at.which < 0) {

@@ -145,30 +145,43 @@ __global__ __launch_bounds__(256) void kv_read_kernel(CacheView c, T* k_out, T* 
   Vec8<T>::store((is_v ? v_out : k_out) + ((int64_t)b * kv_heads + h) * n * DH + at * 8, x);
 }
 
-// Rows of any slots: a thread per 8 elements of a token's row; grid (tokens in blocks, heads of k and v)
+// Rows of any slots: a thread per 16 elements of a token's rows of k and v; grid (tokens in blocks, heads)
 template <typename T, forge_kv_type S, int DH>
 __global__ __launch_bounds__(256) void paged_read_kernel(PagedRows p) {
-  const int h = blockIdx.y >> 1;
-  const bool is_v = blockIdx.y & 1;
-  const uint32_t gid = blockIdx.x * 256u + threadIdx.x, tok = gid / (DH / 8), d = gid % (DH / 8) * 8;
+  const int h = blockIdx.y;
+  const uint32_t gid = blockIdx.x * 256u + threadIdx.x, tok = gid / (DH / 16), d = gid % (DH / 16) * 16;
   if (tok >= (uint32_t)p.tokens) return;
   const int slot = p.slots[tok], shift = p.cache.shift;
   if ((uint32_t)slot >= (uint32_t)p.cache.n_pages << shift) return;
   const CacheView& c = p.cache.c;
   const int64_t e = (slot >> shift) * c.bs + h * c.hs + (int64_t)(slot & ((1 << shift) - 1)) * DH + d;
-  float x[8];
+  T* const ky = reinterpret_cast<T*>(p.k.p) + tok * p.k.ts + h * p.k.hs + d;
+  T* const vy = reinterpret_cast<T*>(p.v.p) + tok * p.v.ts + h * p.v.hs + d;
   if constexpr (S == FORGE_KV_SAME) {
-    Vec8<T>::load(reinterpret_cast<const T*>(is_v ? c.v : c.k) + e, x);
-  } else {
-    const u32x2 w = *reinterpret_cast<const u32x2*>((is_v ? c.v : c.k) + e);
-    const float scale = (is_v ? c.vs : c.ks)[e / DH];
-    Codes<S>::unpack(w[0], x);
-    Codes<S>::unpack(w[1], x + 4);
+    constexpr int N = sizeof(T);           // 16-byte words of 16 elements
+    const u32x4 *kx = reinterpret_cast<const u32x4*>(reinterpret_cast<const T*>(c.k) + e), *vx = reinterpret_cast<const u32x4*>(reinterpret_cast<const T*>(c.v) + e);
+    u32x4 k[N], v[N];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] *= scale;
+    for (int i = 0; i < N; ++i) { k[i] = kx[i]; v[i] = vx[i]; }
+#pragma unroll
+    for (int i = 0; i < N; ++i) { reinterpret_cast<u32x4*>(ky)[i] = k[i]; reinterpret_cast<u32x4*>(vy)[i] = v[i]; }
+  } else {
+    const u32x4 k = *reinterpret_cast<const u32x4*>(c.k + e), v = *reinterpret_cast<const u32x4*>(c.v + e);
+    const float ks = c.ks[e / DH], vs = c.vs[e / DH];
+    auto put = [](T* y, const u32x4& w, float scale) {
+#pragma unroll
+      for (int i = 0; i < 4; i += 2) {
+        float x[8];
+        Codes<S>::unpack(w[i], x);
+        Codes<S>::unpack(w[i + 1], x + 4);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] *= scale;
+        Vec8<T>::store(y + 4 * i, x);
+      }
+    };
+    put(ky, k, ks);
+    put(vy, v, vs);
   }
-  const Heads& y = is_v ? p.v : p.k;
-  Vec8<T>::store(reinterpret_cast<T*>(y.p) + tok * y.ts + h * y.hs + d, x);
 }
 
 // A wave per (layer, sequence, head, k or v) walks over the accepted rows in rising order, ROWS of them at a time.  In place: a
@@ -220,7 +233,7 @@ void read_dh(const CacheView& c, int batch, int kv_heads, int head_dim, void* k_
 
 template <typename T, forge_kv_type S>
 void paged_read_dh(const PagedRows& a, hipStream_t s) {
-  const dim3 grid((unsigned)ceil_div64((int64_t)a.tokens * (a.head_dim / 8), 256), 2 * a.kv_heads);
+  const dim3 grid((unsigned)ceil_div64((int64_t)a.tokens * (a.head_dim / 16), 256), a.kv_heads);
   if (a.head_dim == 64) paged_read_kernel<T, S, 64><<<grid, 256, 0, s>>>(a);
   else paged_read_kernel<T, S, 128><<<grid, 256, 0, s>>>(a);
 }
