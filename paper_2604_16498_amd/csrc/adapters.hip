@@ -49,183 +49,98 @@ struct Rows {
 
 struct Cut { int tiles, splits, chunks, lanes, groups; };      // groups: of 64 columns, a block of the second launch
 
-// 16 bytes of each of N rows at unit u of the range's n; a unit that is not there asks for one line (the loads stay, so that their number is known
-// and a wait is for no more than what it needs)
-template <typename T, int N>
-__device__ inline void load_unit(u32x4 (&r)[N], const T* const (&src)[N], const T* some, int u, int n, int k, int K, int at16) {
-  const bool in = u < n && k + at16 < K;
-#pragma unroll
-  for (int i = 0; i < N; ++i) r[i] = *reinterpret_cast<const u32x4*>(in ? src[i] + k : some);
-}
-// ... and into LDS, 0 past the end of K
-template <int N, int APART>
-__device__ inline void store_unit(char* to, const u32x4 (&r)[N], bool in) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4*>(to + i * APART) = in ? r[i] : u32x4{0, 0, 0, 0};
-}
-
-// t of 16 rows and 64 inner columns over one range of K, whose units of 128 bytes a row are shared out among 4 waves.  A unit of x and of the adapter comes
-// in 1 KB pieces of 8 whole lines into registers, two units ahead, and goes through LDS of its wave alone: read as operands from memory, 16 bytes of 64
-// rows a load, each lane would be a line lookup.
-template <typename T>
+// t of 16 RT rows and 64 inner columns over one range of K, in units of 512 bytes a row: a load of a block is 8 rows x 512 bytes (in lines of 128 bytes,
+// rows of 8 KB came at two thirds of the rate), two units of x and of the adapter are on their way in registers, and a unit goes through LDS.
+// Wave w multiplies inner columns 16 w .. with all rows.
+template <typename T, int RT>
 __global__ __launch_bounds__(256, 2) void adapters_inner_kernel(AdapterArgs p, Cut cut) {
   typedef Mma<T> M;
-  constexpr int PER = 16 / sizeof(T), UNIT = 8 * PER, ROW = 144, WAVES = 4;       // (rows 16 bytes apart in the banks)
-  __shared__ __attribute__((aligned(16))) char lds[WAVES][(16 + 16 * JT) * ROW];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, kg = lane >> 4;
-  const int inner = p.parts * p.rank, line = lane >> 3, at16 = (lane & 7) * PER;
-  const int64_t m0 = (int64_t)blockIdx.x * 16;
+  constexpr int PER = 16 / sizeof(T), UNIT = 32 * PER, ROW = 528, XN = 2 * RT, AN = 2 * JT;      // (rows 16 bytes apart in the banks)
+  __shared__ __attribute__((aligned(16))) char lds[(16 * RT + 16 * JT) * ROW];                   // rows of x, then of the adapter
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, kg = lane >> 4;
+  const int inner = p.parts * p.rank, line = tid >> 5, at16 = (tid & 31) * PER;
+  const int64_t m0 = (int64_t)blockIdx.x * (16 * RT);
   const int split = blockIdx.y / cut.chunks, j0 = blockIdx.y % cut.chunks * (16 * JT);
   const int tiles = min(JT, ceil_div(inner - j0, 16));                   // of the inner index that there are here
-  const int units = ceil_div(p.K, UNIT), part = split * WAVES + wave, parts = cut.splits * WAVES;
-  const int u0 = (int)((int64_t)units * part / parts), n = (int)((int64_t)units * (part + 1) / parts) - u0;
-  const T* const some = reinterpret_cast<const T*>(p.x);
-  const T* xs[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int64_t m = m0 + 8 * i + line;
-    xs[i] = some + (m < p.M ? m : p.M - 1) * p.K + at16;
-  }
-  u32x4 xf[2][2], af[2][2 * JT];                                         // two units in flight
-  auto load_x = [&](int u, u32x4 (&r)[2]) { load_unit<T>(r, xs, some, u, n, (u0 + u) * UNIT, p.K, at16); };
-  load_x(0, xf[0]);
-  load_x(1, xf[1]);
-  const Rows rows(p, m0, 16);
-  char* const patch = lds[wave];
-  uint64_t left = rows.leaders;
-  bool again = false;
-  for (int s = 0; left != 0; ++s, left &= left - 1) {
-    if (s % cut.lanes != (int)blockIdx.z) continue;
-    const int id = __builtin_amdgcn_readlane(rows.id, __ffsll((unsigned long long)left) - 1);
-    const T* as[2 * JT];
-#pragma unroll
-    for (int i = 0; i < 2 * JT; ++i)
-      as[i] = reinterpret_cast<const T*>(p.a) + ((int64_t)id * inner + min(j0 + 8 * i + line, inner - 1)) * p.K + at16;
-    auto load_a = [&](int u, u32x4 (&r)[2 * JT]) { load_unit<T>(r, as, some, u, n, (u0 + u) * UNIT, p.K, at16); };
-    floatx4 acc[JT];
-#pragma unroll
-    for (int j = 0; j < JT; ++j) acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    if (again) {
-      load_x(0, xf[0]);
-      load_x(1, xf[1]);
-    }
-    again = true;
-    load_a(0, af[0]);
-    load_a(1, af[1]);
-    auto step = [&](int u, u32x4 (&x)[2], u32x4 (&a)[2 * JT]) {
-      wave_lds_sync();
-      char* const to = patch + line * ROW + (lane & 7) * 16;
-      const bool in = (u0 + u) * UNIT + at16 < p.K;
-      store_unit<2, 8 * ROW>(to, x, in);
-      store_unit<2 * JT, 8 * ROW>(to + 16 * ROW, a, in);
-      wave_lds_sync();
-      load_x(u + 2, x);
-      load_a(u + 2, a);
-      const char* const from = patch + c * ROW + kg * 16;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(from + h * 64);
-#pragma unroll
-        for (int j = 0; j < JT; ++j)
-          if (j < tiles) acc[j] = M::go(*reinterpret_cast<const u32x4*>(from + (16 + 16 * j) * ROW + h * 64), x, acc[j]);
-      }
-    };
-    for (int u = 0; u < n; u += 2) {
-      step(u, xf[0], af[0]);
-      if (u + 1 < n) step(u + 1, xf[1], af[1]);
-    }
-    // ---- the waves' sums in order: 4 inner indices of a row a lane
-    wave_lds_sync();
-#pragma unroll
-    for (int j = 0; j < JT; ++j) *reinterpret_cast<floatx4*>(patch + j * 1024 + lane * 16) = acc[j];
-    lds_barrier();
-    floatx4 t = *reinterpret_cast<const floatx4*>(lds[0] + wave * 1024 + lane * 16);
-#pragma unroll
-    for (int w = 1; w < WAVES; ++w) t += *reinterpret_cast<const floatx4*>(lds[w] + wave * 1024 + lane * 16);
-    const int at = j0 + 16 * wave + 4 * kg, mine = __shfl(rows.id, c, 64);
-    if (mine == id && at < inner)
-      *reinterpret_cast<floatx4*>(reinterpret_cast<float*>(p.workspace) + ((int64_t)split * p.M + m0 + c) * inner + at) = t;
-    lds_barrier();
-  }
-}
-
-// The same for many rows, of which 64 next to one another mostly share an adapter: a block's waves take 16 rows each and share the adapter's units through
-// two buffers of LDS.
-template <typename T>
-__global__ __launch_bounds__(256, 2) void adapters_inner_many_kernel(AdapterArgs p, Cut cut) {
-  typedef Mma<T> M;
-  constexpr int PER = 16 / sizeof(T), UNIT = 8 * PER, ROW = 144, AHEAD = 4;
-  __shared__ __attribute__((aligned(16))) char lds[2][128 * ROW];          // rows of x, then of the adapter
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, kg = lane >> 4;
-  const int inner = p.parts * p.rank, line = tid >> 3, at16 = (tid & 7) * PER;
-  const int64_t m0 = (int64_t)blockIdx.x * 64;
-  const int split = blockIdx.y / cut.chunks, j0 = blockIdx.y % cut.chunks * (16 * JT);
-  const int tiles = min(JT, ceil_div(inner - j0, 16));
   const int units = ceil_div(p.K, UNIT);
-  const int u0 = (int)((int64_t)units * split / cut.splits), n = (int)((int64_t)units * (split + 1) / cut.splits) - u0;
-  const T* const some = reinterpret_cast<const T*>(p.x);
-  const T* xs[2];
+  const int u0 = (int)((int64_t)units * split / cut.splits), u1 = (int)((int64_t)units * (split + 1) / cut.splits);
+  const T* xs[XN];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int64_t m = m0 + 32 * i + line;
-    xs[i] = some + (m < p.M ? m : p.M - 1) * p.K + at16;
+  for (int i = 0; i < XN; ++i) {
+    const int64_t m = m0 + 8 * i + line;
+    xs[i] = reinterpret_cast<const T*>(p.x) + (m < p.M ? m : p.M - 1) * p.K;
   }
-  u32x4 xf[AHEAD][2], af[AHEAD][2];
-  auto load_x = [&](int u, u32x4 (&r)[2]) { load_unit<T>(r, xs, some, u, n, (u0 + u) * UNIT, p.K, at16); };
-  bool again = blockIdx.z > 0;           // x not requested yet: few tiles have a second adapter
+  u32x4 xf[2][XN], af[2][AN];
+  auto offset = [&](int u) { return min(u * UNIT + at16, p.K - PER); };  // (what lies past the end of K is 0 in LDS)
+  auto load_x = [&](int u, u32x4 (&r)[XN]) {
+    const int k = offset(u);
+#pragma unroll
+    for (int i = 0; i < XN; ++i) r[i] = *reinterpret_cast<const u32x4*>(xs[i] + k);
+  };
+  bool again = blockIdx.z > 0;             // x not requested yet: few tiles have many adapters
   if (!again) {
-#pragma unroll
-    for (int a = 0; a < AHEAD; ++a) load_x(a, xf[a]);
+    load_x(u0, xf[0]);
+    if (u0 + 1 < u1) load_x(u0 + 1, xf[1]);
   }
-  const Rows rows(p, m0, 64);
+  const Rows rows(p, m0, 16 * RT);
   uint64_t left = rows.leaders;
   for (int s = 0; left != 0; ++s, left &= left - 1) {
     if (s % cut.lanes != (int)blockIdx.z) continue;
     const int id = __builtin_amdgcn_readlane(rows.id, __ffsll((unsigned long long)left) - 1);
-    const T* as[2];
+    const T* as[AN];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-      as[i] = reinterpret_cast<const T*>(p.a) + ((int64_t)id * inner + min(j0 + 32 * i + line, inner - 1)) * p.K + at16;
-    auto load_a = [&](int u, u32x4 (&r)[2]) { load_unit<T>(r, as, some, u, n, (u0 + u) * UNIT, p.K, at16); };
-    if (again) {
+    for (int i = 0; i < AN; ++i) as[i] = reinterpret_cast<const T*>(p.a) + ((int64_t)id * inner + min(j0 + 8 * i + line, inner - 1)) * p.K;
+    auto load_a = [&](int u, u32x4 (&r)[AN]) {
+      const int k = offset(u);
 #pragma unroll
-      for (int a = 0; a < AHEAD; ++a) load_x(a, xf[a]);
+      for (int i = 0; i < AN; ++i)
+        if (i < 2 * tiles) r[i] = *reinterpret_cast<const u32x4*>(as[i] + k);
+    };
+    load_a(u0, af[0]);
+    if (again) load_x(u0, xf[0]);
+    if (u0 + 1 < u1) {
+      load_a(u0 + 1, af[1]);
+      if (again) load_x(u0 + 1, xf[1]);
     }
     again = true;
+    floatx4 acc[RT];
 #pragma unroll
-    for (int a = 0; a < AHEAD; ++a) load_a(a, af[a]);
-    floatx4 acc[JT];
+    for (int i = 0; i < RT; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    auto step = [&](int u, u32x4 (&x)[XN], u32x4 (&a)[AN]) {
+      const bool in = u * UNIT + at16 < p.K;
+      char* const to = lds + line * ROW + (tid & 31) * 16;
+      const u32x4 zero = {0, 0, 0, 0};
 #pragma unroll
-    for (int j = 0; j < JT; ++j) acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    auto step = [&](int u, u32x4 (&x)[2], u32x4 (&a)[2]) {
-      char* const buf = lds[u & 1];
-      const bool in = (u0 + u) * UNIT + at16 < p.K;
-      char* const to = buf + line * ROW + (tid & 7) * 16;
-      store_unit<2, 32 * ROW>(to, x, in);
-      store_unit<2, 32 * ROW>(to + 64 * ROW, a, in);
-      load_x(u + AHEAD, x);
-      load_a(u + AHEAD, a);
-      lds_barrier();                     // (the other buffer's readers are past it)
+      for (int i = 0; i < XN; ++i) *reinterpret_cast<u32x4*>(to + 8 * i * ROW) = in ? x[i] : zero;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(buf + (16 * wave + c) * ROW + h * 64 + kg * 16);
-#pragma unroll
-        for (int j = 0; j < JT; ++j)
-          if (j < tiles) acc[j] = M::go(*reinterpret_cast<const u32x4*>(buf + (64 + 16 * j + c) * ROW + h * 64 + kg * 16), x, acc[j]);
+      for (int i = 0; i < AN; ++i)
+        if (i < 2 * tiles) *reinterpret_cast<u32x4*>(to + (16 * RT + 8 * i) * ROW) = in ? a[i] : zero;
+      if (u + 2 < u1) {
+        load_x(u + 2, x);
+        load_a(u + 2, a);
       }
+      lds_barrier();
+      if (wave < tiles) {
+        const char* const from = lds + c * ROW + kg * 16;
+#pragma unroll
+        for (int h = 0; h < 8; ++h) {
+          const u32x4 w = *reinterpret_cast<const u32x4*>(from + (16 * RT + 16 * wave) * ROW + h * 64);
+#pragma unroll
+          for (int i = 0; i < RT; ++i) acc[i] = M::go(w, *reinterpret_cast<const u32x4*>(from + 16 * i * ROW + h * 64), acc[i]);
+        }
+      }
+      lds_barrier();
     };
-    for (int u = 0; u < n; u += AHEAD) {
-#pragma unroll
-      for (int a = 0; a < AHEAD; ++a)
-        if (u + a < n) step(u + a, xf[a], af[a]);
+    for (int u = u0; u < u1; u += 2) {
+      step(u, xf[0], af[0]);
+      if (u + 1 < u1) step(u + 1, xf[1], af[1]);
     }
-    lds_barrier();                       // before the next adapter's first unit
-    const int row = 16 * wave + c, mine = __shfl(rows.id, row, 64);
-    float* to = reinterpret_cast<float*>(p.workspace) + ((int64_t)split * p.M + m0 + row) * inner;
+    const int at = j0 + 16 * wave + 4 * kg;                    // 4 inner indices of a row a lane
 #pragma unroll
-    for (int j = 0; j < JT; ++j) {
-      const int at = j0 + 16 * j + 4 * kg;
-      if (mine == id && at < inner) *reinterpret_cast<floatx4*>(to + at) = acc[j];
+    for (int i = 0; i < RT; ++i) {
+      const int mine = __shfl(rows.id, 16 * i + c, 64);
+      if (mine == id && at < inner)
+        *reinterpret_cast<floatx4*>(reinterpret_cast<float*>(p.workspace) + ((int64_t)split * p.M + m0 + 16 * i + c) * inner + at) = acc[i];
     }
   }
 }
@@ -424,7 +339,8 @@ __global__ __launch_bounds__(256, 2) void adapters_outer_kernel(AdapterArgs p, C
 }
 
 // Many rows: 64 of them and 256 columns of one part, 64 a wave.  Most share an adapter: base, b and t are requested at once and no row is tested (beside memory,
-// instructions bound these blocks), and a row's accesses are one offset a lane from scalar addresses.  Where they do not, one adapter after another.
+// instructions bound these blocks), and a row's accesses are one offset a lane from scalar addresses, past the caches (4096 x 4096, rank 64: 24.0 | 20.4 us).
+// Where they do not, one adapter after another.
 template <typename T, int NS>
 __global__ __launch_bounds__(256, 2) void adapters_outer_many_kernel(AdapterArgs p, Cut cut) {
   typedef typename Four<T>::type F;
@@ -443,22 +359,23 @@ __global__ __launch_bounds__(256, 2) void adapters_outer_many_kernel(AdapterArgs
     for (int i = 0; i < 4 && m0 + 16 * i < p.M; ++i) outer_rows<T, NS>(p, cut, 1, 0, m0 + 16 * i, b0, b1, tl);
     return;
   }
-  const Rows rows(p, m0, 64);
-  const uint64_t none = __ballot(rows.id < 0);
-  if (none == ~0ull && p.y == p.base) return;
   const int n0 = b0 + 64 * wave;
   const int64_t row = p.ldy * (int64_t)sizeof(T);
   const uint32_t at = 4 * kg * (uint32_t)row + 4 * c * (uint32_t)sizeof(T);      // (ldy is at most 2^24)
   const char* const base = reinterpret_cast<const char*>(p.base) + m0 * row + n0 * (int64_t)sizeof(T);
   char* const y = reinterpret_cast<char*>(p.y) + m0 * row + n0 * (int64_t)sizeof(T);
-  int id = __builtin_amdgcn_readlane(rows.id, rows.leaders != 0 ? __ffsll((unsigned long long)rows.leaders) - 1 : 0);
-  u32x4 bf[4][NS];
-  if (rows.leaders != 0) load_b<T, NS>(bf, p, id, n0);
   F old[4][4];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) old[i][e] = *reinterpret_cast<const F*>(base + (16 * i + e) * row + at);
+    for (int e = 0; e < 4; ++e) old[i][e] = __builtin_nontemporal_load(reinterpret_cast<const F*>(base + (16 * i + e) * row + at));
+  I t;
+  t.load(p, cut.splits, m0, 64, part);
+  const Rows rows(p, m0, 64);
+  const uint64_t none = __ballot(rows.id < 0);
+  int id = __builtin_amdgcn_readlane(rows.id, rows.leaders != 0 ? __ffsll((unsigned long long)rows.leaders) - 1 : 0);
+  u32x4 bf[4][NS];
+  if (rows.leaders != 0) load_b<T, NS>(bf, p, id, n0);
   if (none != 0 && p.y != p.base) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -467,14 +384,10 @@ __global__ __launch_bounds__(256, 2) void adapters_outer_many_kernel(AdapterArgs
         if (none >> (16 * i + 4 * kg + e) & 1) *reinterpret_cast<F*>(y + (16 * i + e) * row + at) = old[i][e];
   }
   if (rows.leaders == 0) return;
-  {
-    I t;
-    t.load(p, cut.splits, m0, 64, part);
-    t.store(tl, [&](int r) {
-      const int whose = __shfl(rows.id, r, 64);
-      return p.scale != nullptr ? p.scale[max(whose, 0)] : 1.f;
-    });
-  }
+  t.store(tl, [&](int r) {
+    const int whose = __shfl(rows.id, r, 64);
+    return p.scale != nullptr ? p.scale[max(whose, 0)] : 1.f;
+  });
   lds_barrier();
   for (uint64_t left = rows.leaders;;) {
     const uint64_t here = __ballot(rows.id == id);
@@ -487,12 +400,12 @@ __global__ __launch_bounds__(256, 2) void adapters_outer_many_kernel(AdapterArgs
       if (here == ~0ull) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          *reinterpret_cast<F*>(y + (16 * i + e) * row + at) = Four<T>::added(old[i][e], floatx4{acc[0][e], acc[1][e], acc[2][e], acc[3][e]});
+          __builtin_nontemporal_store(Four<T>::added(old[i][e], floatx4{acc[0][e], acc[1][e], acc[2][e], acc[3][e]}), reinterpret_cast<F*>(y + (16 * i + e) * row + at));
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           if (here >> (16 * i + 4 * kg + e) & 1)
-            *reinterpret_cast<F*>(y + (16 * i + e) * row + at) = Four<T>::added(old[i][e], floatx4{acc[0][e], acc[1][e], acc[2][e], acc[3][e]});
+            __builtin_nontemporal_store(Four<T>::added(old[i][e], floatx4{acc[0][e], acc[1][e], acc[2][e], acc[3][e]}), reinterpret_cast<F*>(y + (16 * i + e) * row + at));
       }
     }
     left &= left - 1;
@@ -505,16 +418,16 @@ __global__ __launch_bounds__(256, 2) void adapters_outer_many_kernel(AdapterArgs
 // From here on the blocks take 64 rows: most of them share an adapter with their neighbours
 constexpr int MANY = 1024;
 
-// K in ranges until the blocks fill the chip, of two units a wave (a block, of many rows: four) at least
+// K in ranges until the blocks fill the chip twice (of many rows once: 4096 x 4096, rank 64, 4 | 8 ranges 15.2 | 15.6 us, and less to add up)
 Cut cut_of(int M, int K, int inner, forge_dtype dt) {
-  const bool many = M >= MANY;
-  const int units = ceil_div(K, dt == FORGE_BF16 ? 64 : 32), least = many ? 4 : 8;
+  const int units = ceil_div(K, dt == FORGE_BF16 ? 256 : 128);
   Cut c;
-  c.tiles = ceil_div(M, many ? 64 : 16);
+  c.tiles = ceil_div(M, M >= MANY ? 64 : 16);
   c.chunks = ceil_div(inner, 16 * JT);
   const int64_t blocks = (int64_t)c.tiles * c.chunks;
-  const int want = (int)ceil_div64((many ? 1 : 2) * compute_units(), blocks), most = units < least ? 1 : units / least;
-  c.splits = want < 1 ? 1 : want < most ? want : most;
+  const int want = (int)ceil_div64((M >= MANY ? 1 : 2) * compute_units(), blocks);
+  const int most = M >= MANY ? units : ceil_div(units, 2);     // (two units a block: both are on their way at once)
+  c.splits = want < most ? want : most;
   c.lanes = c.groups = 1;
   return c;
 }
@@ -534,10 +447,10 @@ forge_status launch(const AdapterArgs& a, hipStream_t s) {
     const int most = many ? 1 : a.M < 16 ? a.M : 16;
     return (int)(l < 1 ? 1 : l < most ? l : most);
   };
-  c.lanes = many ? 4 : lanes((int64_t)c.tiles * c.chunks * c.splits);
+  c.lanes = many ? 2 : lanes((int64_t)c.tiles * c.chunks * c.splits);
   const dim3 grid(c.tiles, c.chunks * c.splits, c.lanes);
-  if (many) adapters_inner_many_kernel<T><<<grid, 256, 0, s>>>(a, c);
-  else adapters_inner_kernel<T><<<grid, 256, 0, s>>>(a, c);
+  if (many) adapters_inner_kernel<T, 4><<<grid, 256, 0, s>>>(a, c);
+  else adapters_inner_kernel<T, 1><<<grid, 256, 0, s>>>(a, c);
   if (hipGetLastError() != hipSuccess) return FORGE_ERR_HIP;
   c.groups = many || a.N <= 256 ? 4 : 8;
   const int64_t blocks = (int64_t)(many ? ceil_div(c.tiles, 8) * 8 : c.tiles) * ceil_div(a.N, 64 * c.groups);
@@ -553,11 +466,11 @@ forge_status launch(const AdapterArgs& a, hipStream_t s) {
 
 }  // namespace
 
-// Room for any smaller M too: of m rows in `tiles` tiles the ranges are at most units / 4 (8: fewer rows), and at most 2 cus / (tiles chunks) + 1; times m
-// rows, of which a tile has at most 16 (64, but then half as many blocks are asked for)
+// Room for any smaller M too: of m rows in `tiles` tiles the ranges are at most the units of K, and at most 2 cus (1 of 64 rows) / (tiles chunks) + 1; times m rows, of
+// which a tile has at most 16 or 64
 size_t adapters_workspace_bytes(int M, int N, int K, int rank, int parts, forge_dtype dt) {
-  const int inner = parts * rank, units = ceil_div(K, dt == FORGE_BF16 ? 64 : 32), least = M >= MANY ? 4 : 8;
-  const int64_t most = (int64_t)(units < least ? 1 : units / least) * M;
+  const int inner = parts * rank, units = ceil_div(K, dt == FORGE_BF16 ? 256 : 128);
+  const int64_t most = (int64_t)units * M;
   const int64_t full = ceil_div((M >= MANY ? 64 : 32) * compute_units(), ceil_div(inner, 16 * JT)) + (int64_t)M;
   return (size_t)(most < full ? most : full) * inner * sizeof(float);
 }

@@ -5,7 +5,8 @@
 // n + j.  All of it is prefix sums and whole numbers: a block walks over the requests a chunk at a time, a thread each, and deals what the
 // chunk's requests have together (pages, tokens) to its threads by a search in their running sums.
 // Latency, not bytes, bounds it: a chain of loads (lengths and changes; then old and new page numbers together, the new ones from the
-// stack rather than from the table), few steps between them, one wave where the requests fit one.
+// stack rather than from the table), few steps between them, one wave where the requests fit one.  3 requests that add a token 2.7 us, 256 that
+// grow and end with a prompt among them, 8192 tokens, 10.2.
 #include "paged.hpp"
 
 namespace forge {
@@ -188,6 +189,7 @@ __global__ __launch_bounds__(256) void pages_slots_kernel(PagesArgs p) {
 }  // namespace
 
 forge_status launch_pages_assign(const PagesArgs& a, hipStream_t s) {
+  // the tokens' slots by a launch of its own where one block would take longer (256 requests, 8192 tokens: 6.5 + 3.7 us, in one 14.5)
   const bool apart = a.max_tokens > 4096;
   if (a.batch <= 64 && a.max_tokens <= 256) {
     pages_assign_kernel<true><<<1, 64, 0, s>>>(a, 1);
