@@ -531,7 +531,7 @@ forge_status forge_paged_read(const forge_paged_cache* cache, int layer, const f
 /* Attention of one new token per request over layer `layer`, its row already appended:
  *   out[b, h*dh : (h+1)*dh] = sum_j P[b,h,j] v[b, g(h), j, :],  P = softmax over the rows j < lengths[b] of scale * q[b,h] . k[b,g(h),j]
  * lengths: DEVICE int32 [batch], clamped to [0, max_len]; a request of length 0 (an idle place) gets zeros.  max_len: HOST, 1 ..
- * table_cols * page_rows, sizes the launch and the workspace.  table: DEVICE int32 [batch, table_cols]; entries are clamped to
+ * table_cols * page_rows and at most 2^30, sizes the launch and the workspace.  table: DEVICE int32 [batch, table_cols]; entries are clamped to
  * [0, n_pages), so that a bad one gives a wrong result for that request, never an access outside the pool; those past a request's last
  * row are not used.  What lies in rows behind a length, infinities and NaN among it, does not reach the output.
  * q: [batch, head, head_dim] view (its token_stride is not looked at); out: [batch, q_heads * head_dim] dense, in dt.  fp32 scores, statistics and

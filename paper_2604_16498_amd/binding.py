@@ -660,6 +660,12 @@ def make_page_pool(free_pages, free_count, table, page_rows) -> PagePool:
     return p
 
 
+def _here(t: torch.Tensor):
+    """The work goes to the current device's stream: its tensors have to lie there."""
+    if t.get_device() != _device():
+        raise ValueError("the tensors are on GPU %d, the current one is %d" % (t.get_device(), _device()))
+
+
 def _vector(t: torch.Tensor, n: int, what: str):
     if t.dtype is not _INT32 or t.numel() != n or not t.is_cuda or not t.is_contiguous():
         raise ValueError("%s must be a contiguous int32 GPU tensor of %d entries" % (what, n))
@@ -670,6 +676,7 @@ def forge_pages_assign(pool: PagePool, lengths, change, lengths_out, granted, st
     """Lengths change by change[b] (int32 [batch]), pages move, and every new token gets slots, positions and owners (int32
     [max_tokens], or all None); granted [batch]: the changes that took place; starts [batch + 1]: the tokens of every request."""
     B = pool.batch
+    _here(lengths)
     if slots is None:
         if positions is not None or owners is not None:
             raise ValueError("slots, positions and owners come together")
@@ -706,6 +713,7 @@ def _rows(t: torch.Tensor) -> Heads:
 def forge_paged_append(cache: PagedCache, k, v, slots, rope=None, positions=None, q=None, q_out=None, layer=0):
     """k, v [T,Hkv,dh] views into the rows of slots [T], k rotated at positions [T]; q [T,Hq,dh] rotated into q_out (may be q)."""
     T, heads, dh = k.shape
+    _here(k)
     if heads != cache.kv_heads or dh != cache.head_dim or v.shape != k.shape:
         raise ValueError("k and v must be [T, %d, %d]" % (cache.kv_heads, cache.head_dim))
     if (q is None) != (q_out is None) or slots is None:
@@ -727,6 +735,7 @@ def forge_paged_append(cache: PagedCache, k, v, slots, rope=None, positions=None
 def forge_paged_read(cache: PagedCache, k_out, v_out, slots, layer=0):
     """k_out, v_out [T,Hkv,dh] views: the rows of slots [T] as values in the cache's activation type."""
     T, heads, dh = k_out.shape
+    _here(k_out)
     if (heads, dh) != (cache.kv_heads, cache.head_dim) or v_out.shape != k_out.shape or slots is None:
         raise ValueError("k_out and v_out must be [T, %d, %d]" % (cache.kv_heads, cache.head_dim))
     _cache_dt(cache, k_out, v_out)
@@ -745,8 +754,11 @@ def forge_attn_paged(cache: PagedCache, q, out, lengths, table, max_len, scale=N
     if dh != cache.head_dim or out.shape != (B, H * dh) or lengths is None or table.dim() != 2:
         raise ValueError("q must be [B, Hq, %d], out [B, Hq * %d], table [B, cols]" % (cache.head_dim, cache.head_dim))
     _cache_dt(cache, q, out)
-    view = _rows(q)
-    view.batch_stride, view.token_stride = view.token_stride, 0
+    sb, sh, sd = q.stride()
+    if not q.is_cuda or (sd != 1 and dh != 1):
+        raise ValueError("forge needs [request, head, head_dim] GPU tensors with a dense last axis")
+    _here(q)
+    view = Heads(q.data_ptr(), sb, 0, sh)
     wp, wb = _ws(workspace)
     _check(lib().forge_attn_paged(C.byref(cache), layer, C.byref(view), _p(out), _vector(lengths, B, "lengths"),
                                   _int32(table, (B, table.shape[1]), "table"), table.shape[1], H, B, max_len,
@@ -773,6 +785,7 @@ def forge_adapters_workspace_bytes(adapters: Adapters, M) -> int:
 def forge_adapters_add(adapters: Adapters, x, base, y, ids, workspace=None):
     """y[m, :N] = base[m, :N] + the adapter ids[m] of x[m] (none where it is outside the range); y may be base, and both wider than N."""
     M, K = x.shape
+    _here(x)
     if K != adapters.K or base.shape != y.shape or y.shape[0] != M or ids is None:
         raise ValueError("x must be [M, %d], base and y [M, at least %d]" % (adapters.K, adapters.N))
     if not x.dtype == base.dtype == y.dtype or _dt(x) != adapters.dt:

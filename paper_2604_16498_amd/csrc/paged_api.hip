@@ -48,7 +48,7 @@ bool is_cache(const forge_paged_cache* c, const void* p) { return p == c->k || p
 // the attention's blocks, a (request, cache head) and 16 query heads each, rounded up to whole turns of the XCDs, are a 32-bit grid
 forge_status check_attn(const forge_paged_cache* c, int q_heads, int batch, int max_len) {
   if (q_heads < 1 || q_heads % c->kv_heads != 0 || batch < 1 || max_len < 1) return FORGE_ERR_INVALID_ARG;
-  if (q_heads > kMaxGridDim || batch > kMaxGridDim ||
+  if (q_heads > kMaxGridDim || batch > kMaxGridDim || max_len > 1 << 30 ||
       ((int64_t)batch * c->kv_heads + 8) * ceil_div(q_heads / c->kv_heads, 16) >= ((int64_t)1 << 24))
     return FORGE_ERR_UNSUPPORTED;
   return FORGE_OK;

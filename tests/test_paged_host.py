@@ -52,7 +52,7 @@ def test_refusals_of_rows_and_attention():
                        (dict(out=None), 1), (dict(out=vp(0x70008)), 1), (dict(out=vp(0x50000)), 1), (dict(out=vp(0x10000)), 1),
                        (dict(lens=None), 1), (dict(lens=vp(0x70002)), 1), (dict(table=None), 1), (dict(table=vp(0x70001)), 1),
                        (dict(q=_heads(ptr=0)), 1), (dict(q=_heads(ptr=0x50008)), 1), (dict(q=_heads(bs=1028)), 1), (dict(q=_heads(hs=-64)), 1),
-                       (dict(hq=80000), 2), (dict(batch=70000), 2), (dict(cols=1 << 27, most=10), 2)):
+                       (dict(hq=80000), 2), (dict(batch=70000), 2), (dict(cols=1 << 27, most=10), 2), (dict(cols=(1 << 27) - 1, most=(1 << 30) + 1), 2)):
         assert attn(**kw) == status, kw
     assert attn(cols=1000, most=16000) == 3                              # its shares need a workspace
     app = lambda r=None, k=x, v=x, q=None, qo=None, hq=0, slots=p, pos=None, n=4, layer=0: l.forge_paged_append(
