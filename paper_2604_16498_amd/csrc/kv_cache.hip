@@ -145,42 +145,62 @@ __global__ __launch_bounds__(256) void kv_read_kernel(CacheView c, T* k_out, T* 
   Vec8<T>::store((is_v ? v_out : k_out) + ((int64_t)b * kv_heads + h) * n * DH + at * 8, x);
 }
 
-// Rows of any slots: a thread per 16 elements of a token's rows of k and v; grid (tokens in blocks, heads)
+// Rows of any slots: a thread per 8 elements of k and v of two tokens, so that stores are whole lines; grid (tokens in blocks, heads)
 template <typename T, forge_kv_type S, int DH>
 __global__ __launch_bounds__(256) void paged_read_kernel(PagedRows p) {
-  const int h = blockIdx.y;
-  const uint32_t gid = blockIdx.x * 256u + threadIdx.x, tok = gid / (DH / 16), d = gid % (DH / 16) * 16;
-  if (tok >= (uint32_t)p.tokens) return;
-  const int slot = p.slots[tok], shift = p.cache.shift;
-  if ((uint32_t)slot >= (uint32_t)p.cache.n_pages << shift) return;
+  constexpr int ITEMS = DH / 8, ROWS = 256 / ITEMS;
+  const int h = blockIdx.y, d = threadIdx.x % ITEMS * 8, shift = p.cache.shift;
   const CacheView& c = p.cache.c;
-  const int64_t e = (slot >> shift) * c.bs + h * c.hs + (int64_t)(slot & ((1 << shift) - 1)) * DH + d;
-  T* const ky = reinterpret_cast<T*>(p.k.p) + tok * p.k.ts + h * p.k.hs + d;
-  T* const vy = reinterpret_cast<T*>(p.v.p) + tok * p.v.ts + h * p.v.hs + d;
+  int64_t e[2];
+  int tok[2];
+  bool live[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    tok[i] = blockIdx.x * (2 * ROWS) + i * ROWS + threadIdx.x / ITEMS;
+    const int slot = tok[i] < p.tokens ? p.slots[tok[i]] : -1;
+    live[i] = (uint32_t)slot < (uint32_t)p.cache.n_pages << shift;
+    e[i] = live[i] ? (slot >> shift) * c.bs + h * c.hs + (int64_t)(slot & ((1 << shift) - 1)) * DH + d : 0;
+  }
   if constexpr (S == FORGE_KV_SAME) {
-    constexpr int N = sizeof(T);           // 16-byte words of 16 elements
-    const u32x4 *kx = reinterpret_cast<const u32x4*>(reinterpret_cast<const T*>(c.k) + e), *vx = reinterpret_cast<const u32x4*>(reinterpret_cast<const T*>(c.v) + e);
-    u32x4 k[N], v[N];
+    Raw8<T> k[2], v[2];
 #pragma unroll
-    for (int i = 0; i < N; ++i) { k[i] = kx[i]; v[i] = vx[i]; }
+    for (int i = 0; i < 2; ++i) {
+      k[i].load(reinterpret_cast<const T*>(c.k) + e[i]);
+      v[i].load(reinterpret_cast<const T*>(c.v) + e[i]);
+    }
 #pragma unroll
-    for (int i = 0; i < N; ++i) { reinterpret_cast<u32x4*>(ky)[i] = k[i]; reinterpret_cast<u32x4*>(vy)[i] = v[i]; }
+    for (int i = 0; i < 2; ++i) {
+      if (!live[i]) continue;
+      float x[8];
+      k[i].values(x);
+      Vec8<T>::store(reinterpret_cast<T*>(p.k.p) + tok[i] * p.k.ts + h * p.k.hs + d, x);
+      v[i].values(x);
+      Vec8<T>::store(reinterpret_cast<T*>(p.v.p) + tok[i] * p.v.ts + h * p.v.hs + d, x);
+    }
   } else {
-    const u32x4 k = *reinterpret_cast<const u32x4*>(c.k + e), v = *reinterpret_cast<const u32x4*>(c.v + e);
-    const float ks = c.ks[e / DH], vs = c.vs[e / DH];
-    auto put = [](T* y, const u32x4& w, float scale) {
+    u32x2 k[2], v[2];
+    float ks[2], vs[2];
 #pragma unroll
-      for (int i = 0; i < 4; i += 2) {
-        float x[8];
-        Codes<S>::unpack(w[i], x);
-        Codes<S>::unpack(w[i + 1], x + 4);
+    for (int i = 0; i < 2; ++i) {
+      k[i] = *reinterpret_cast<const u32x2*>(c.k + e[i]);
+      v[i] = *reinterpret_cast<const u32x2*>(c.v + e[i]);
+      ks[i] = c.ks[e[i] / DH];
+      vs[i] = c.vs[e[i] / DH];
+    }
+    auto put = [](T* y, const u32x2& w, float scale) {
+      float x[8];
+      Codes<S>::unpack(w[0], x);
+      Codes<S>::unpack(w[1], x + 4);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] *= scale;
-        Vec8<T>::store(y + 4 * i, x);
-      }
+      for (int j = 0; j < 8; ++j) x[j] *= scale;
+      Vec8<T>::store(y, x);
     };
-    put(ky, k, ks);
-    put(vy, v, vs);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (!live[i]) continue;
+      put(reinterpret_cast<T*>(p.k.p) + tok[i] * p.k.ts + h * p.k.hs + d, k[i], ks[i]);
+      put(reinterpret_cast<T*>(p.v.p) + tok[i] * p.v.ts + h * p.v.hs + d, v[i], vs[i]);
+    }
   }
 }
 
@@ -233,7 +253,7 @@ void read_dh(const CacheView& c, int batch, int kv_heads, int head_dim, void* k_
 
 template <typename T, forge_kv_type S>
 void paged_read_dh(const PagedRows& a, hipStream_t s) {
-  const dim3 grid((unsigned)ceil_div64((int64_t)a.tokens * (a.head_dim / 16), 256), a.kv_heads);
+  const dim3 grid((unsigned)ceil_div64((int64_t)a.tokens * (a.head_dim / 8), 512), a.kv_heads);
   if (a.head_dim == 64) paged_read_kernel<T, S, 64><<<grid, 256, 0, s>>>(a);
   else paged_read_kernel<T, S, 128><<<grid, 256, 0, s>>>(a);
 }
