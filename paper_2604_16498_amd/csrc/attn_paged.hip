@@ -96,9 +96,9 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 && (S != FORGE_KV_SAME || D
       return from + e[i / HALF] * BYTES + i % HALF * 1024 + l * 16;
     };
 #pragma unroll
-    for (int i = 0; i < L::LOADS; ++i) rk[i] = *reinterpret_cast<const u32x4*>(piece(p.c.k, i));
+    for (int i = 0; i < L::LOADS; ++i) rk[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(piece(p.c.k, i)));
 #pragma unroll
-    for (int i = 0; i < L::LOADS; ++i) rv[i] = *reinterpret_cast<const u32x4*>(piece(p.c.v, i));
+    for (int i = 0; i < L::LOADS; ++i) rv[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(piece(p.c.v, i)));
     if constexpr (SCALED) rs = (lane < TILE ? p.c.ks : p.c.vs)[e[(lane >> 4) & 1] / DH + (l & 15)];
     __builtin_amdgcn_sched_barrier(0);
   };
