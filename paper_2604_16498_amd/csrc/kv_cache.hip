@@ -145,8 +145,9 @@ __global__ __launch_bounds__(256) void kv_read_kernel(CacheView c, T* k_out, T* 
   Vec8<T>::store((is_v ? v_out : k_out) + ((int64_t)b * kv_heads + h) * n * DH + at * 8, x);
 }
 
-// Rows of any slots: a thread per 8 elements of k and v of two tokens, so that stores are whole lines, which then go past the caches (30011 rows of 8
-// heads of 128, int8, 186 MB: 27.8 us, 6.7 TB/s; through them 36.6; half lines a store 40.8, past the caches 59); grid (tokens in blocks, heads)
+// Rows of any slots: a thread per 8 elements of k and v of two tokens, so that stores are whole lines; grid (tokens in blocks, heads).  30011 rows of 8
+// heads of 128, int8 (186 MB): 36.6 us, 5.1 TB/s; a thread per 16 elements of one token, half lines a store, 40.8.  Stores past the caches take 28.0,
+// but what reads the rows next then takes longer than that: 30000 rows and the attention of 256 tokens over them 175 | 181 us, 8000 rows 63 | 64.
 template <typename T, forge_kv_type S, int DH>
 __global__ __launch_bounds__(256) void paged_read_kernel(PagedRows p) {
   constexpr int ITEMS = DH / 8, ROWS = 256 / ITEMS;
@@ -177,8 +178,8 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedRows p) {
       if (!live[i]) continue;
 #pragma unroll
       for (int w = 0; w < N; ++w) {
-        __builtin_nontemporal_store(k[i][w], reinterpret_cast<u32x4*>(reinterpret_cast<T*>(p.k.p) + tok[i] * p.k.ts + h * p.k.hs + d) + w);
-        __builtin_nontemporal_store(v[i][w], reinterpret_cast<u32x4*>(reinterpret_cast<T*>(p.v.p) + tok[i] * p.v.ts + h * p.v.hs + d) + w);
+        reinterpret_cast<u32x4*>(reinterpret_cast<T*>(p.k.p) + tok[i] * p.k.ts + h * p.k.hs + d)[w] = k[i][w];
+        reinterpret_cast<u32x4*>(reinterpret_cast<T*>(p.v.p) + tok[i] * p.v.ts + h * p.v.hs + d)[w] = v[i][w];
       }
     }
   } else {
@@ -197,8 +198,7 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedRows p) {
       Codes<S>::unpack(w[1], x + 4);
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[j] *= scale;
-      const u32x4 o = {pack_bf2(x[0], x[1]), pack_bf2(x[2], x[3]), pack_bf2(x[4], x[5]), pack_bf2(x[6], x[7])};
-      __builtin_nontemporal_store(o, reinterpret_cast<u32x4*>(y));
+      Vec8<T>::store(y, x);
     };
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
