@@ -146,8 +146,9 @@ __global__ __launch_bounds__(256) void kv_read_kernel(CacheView c, T* k_out, T* 
 }
 
 // Rows of any slots: a thread per 8 elements of k and v of two tokens, so that stores are whole lines; grid (tokens in blocks, heads).  30011 rows of 8
-// heads of 128, int8 (186 MB): 36.6 us, 5.1 TB/s; a thread per 16 elements of one token, half lines a store, 40.8.  Stores past the caches take 28.0,
-// but what reads the rows next then takes longer than that: 30000 rows and the attention of 256 tokens over them 175 | 181 us, 8000 rows 63 | 64.
+// heads of 128, int8 (186 MB): 34.3 us, 5.4 TB/s; the rows through the caches 36.6, a thread per 16 elements of one token, half lines a store, 40.8.
+// Stores past the caches too take 28.0, but what reads the rows next then takes longer than they save: 30000 rows and the attention of 256 tokens over
+// them 175 | 181 us, 8000 rows 63 | 64.
 template <typename T, forge_kv_type S, int DH>
 __global__ __launch_bounds__(256) void paged_read_kernel(PagedRows p) {
   constexpr int ITEMS = DH / 8, ROWS = 256 / ITEMS;
@@ -170,8 +171,8 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedRows p) {
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int w = 0; w < N; ++w) {
-        k[i][w] = reinterpret_cast<const u32x4*>(reinterpret_cast<const T*>(c.k) + e[i])[w];
-        v[i][w] = reinterpret_cast<const u32x4*>(reinterpret_cast<const T*>(c.v) + e[i])[w];
+        k[i][w] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(reinterpret_cast<const T*>(c.k) + e[i]) + w);
+        v[i][w] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(reinterpret_cast<const T*>(c.v) + e[i]) + w);
       }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -187,8 +188,8 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedRows p) {
     float ks[2], vs[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      k[i] = *reinterpret_cast<const u32x2*>(c.k + e[i]);
-      v[i] = *reinterpret_cast<const u32x2*>(c.v + e[i]);
+      k[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(c.k + e[i]));
+      v[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(c.v + e[i]));
       ks[i] = c.ks[e[i] / DH];
       vs[i] = c.vs[e[i] / DH];
     }
