@@ -3,8 +3,10 @@
 // Two launches: t = A x into fp32 planes (K in `splits` ranges), then y from their sum in order.  Both work on tiles of 16 rows of x with
 // matrix instructions, one adapter of a tile at a time: rows of other requests are multiplied along, their results dropped (so that no
 // infinity of one request's adapter reaches another's rows).  Neighbours in a batch of requests have different adapters, so a tile's adapters are dealt
-// over blocks (`lanes`) where there are few tiles; the rows of a prompt share one, and blocks then take several tiles.
-// An adapter is read once per tile that has it, which is what bounds a decode step; the rows of x, base and y bound a prompt.
+// over blocks (`lanes`) where there are few tiles; the rows of a prompt share one, and blocks then take 64 of them.
+// An adapter is read once per tile that has it: with the chain adapter number, adapter, sum of each launch that bounds a decode step (61 rows, 49 adapters
+// of rank 16 beside q, k and v of 4096: 8 + 8.6 us for 19 + 10 MB of adapters).  The rows of x, base and y bound a prompt (4096 rows of 5 requests, rank 64,
+// 4096 x 4096: 16.6 + 23 us for 34 + 67 MB; one row of 768 in fp32 4.3 + 4.9).
 #include "paged.hpp"
 
 namespace forge {
@@ -49,9 +51,9 @@ struct Rows {
 
 struct Cut { int tiles, splits, chunks, lanes, groups; };      // groups: of 64 columns, a block of the second launch
 
-// t of 16 RT rows and 64 inner columns over one range of K, in units of 512 bytes a row: a load of a block is 8 rows x 512 bytes (in lines of 128 bytes,
-// rows of 8 KB came at two thirds of the rate), two units of x and of the adapter are on their way in registers, and a unit goes through LDS.
-// Wave w multiplies inner columns 16 w .. with all rows.
+// t of 16 RT rows and 64 inner columns over one range of K, in units of 512 bytes a row: a load of a block is 8 rows x 512 bytes (a kernel that only
+// read 4096 rows of 8 KB took 7.9 us so, 12.0 in lines of 128 bytes), two units of x and of the adapter are on their way in registers, and a unit
+// goes through LDS.  Wave w multiplies inner columns 16 w .. with all rows.
 template <typename T, int RT>
 __global__ __launch_bounds__(256, 2) void adapters_inner_kernel(AdapterArgs p, Cut cut) {
   typedef Mma<T> M;
