@@ -35,9 +35,12 @@ template <> struct Mma<float> {
 struct Rows {
   int id;                // of this lane's row, -1: none
   uint64_t leaders;
-  __device__ inline Rows(const AdapterArgs& p, int64_t m0, int rows) {
+  // what a block asks for first (a wait is for everything that was asked for before)
+  static __device__ inline int request(const AdapterArgs& p, int64_t m0, int rows) {
     const int lane = threadIdx.x & 63;
-    id = lane < rows && m0 + lane < p.M ? p.ids[m0 + lane] : -1;
+    return lane < rows && m0 + lane < p.M ? p.ids[m0 + lane] : -1;
+  }
+  __device__ inline Rows(const AdapterArgs& p, int requested) : id(requested) {
     if ((uint32_t)id >= (uint32_t)p.n_adapters) id = -1;
     uint64_t todo = __ballot(id >= 0);
     leaders = 0;
@@ -49,7 +52,8 @@ struct Rows {
   }
 };
 
-struct Cut { int tiles, splits, chunks, lanes, groups; };      // groups: of 64 columns, a block of the second launch
+// groups: of 64 columns, a block of the second launch; first: tile of 16 rows that it begins with
+struct Cut { int tiles, splits, chunks, lanes, groups, first; };
 
 // t of 16 RT rows and 64 inner columns over one range of K, in units of 512 bytes a row: a load of a block is 8 rows x 512 bytes (a kernel that only
 // read 4096 rows of 8 KB took 7.9 us so, 12.0 in lines of 128 bytes), two units of x and of the adapter are on their way in registers, and a unit
@@ -79,12 +83,15 @@ __global__ __launch_bounds__(256, 2) void adapters_inner_kernel(AdapterArgs p, C
 #pragma unroll
     for (int i = 0; i < XN; ++i) r[i] = *reinterpret_cast<const u32x4*>(xs[i] + k);
   };
+  int ids = 0;                             // (ahead of x where x is long; few rows wait less for x first: 61 rows 15.5 | 15.9 us)
+  if (RT > 1) ids = Rows::request(p, m0, 16 * RT);
   bool again = blockIdx.z > 0;             // x not requested yet: few tiles have many adapters
   if (!again) {
     load_x(u0, xf[0]);
     if (u0 + 1 < u1) load_x(u0 + 1, xf[1]);
   }
-  const Rows rows(p, m0, 16 * RT);
+  if (RT == 1) ids = Rows::request(p, m0, 16);
+  const Rows rows(p, ids);
   uint64_t left = rows.leaders;
   for (int s = 0; left != 0; ++s, left &= left - 1) {
     if (s % cut.lanes != (int)blockIdx.z) continue;
@@ -160,22 +167,25 @@ template <> struct Four<bf16> {
   }
 };
 
-// t of `rows` rows of one part, added up over the ranges: fours of a row's inner indices, thread q % THREADS has four q
+// t of ROWS rows of one part, added up over the ranges: fours of a row's inner indices, thread q % 256 has four q
 template <typename T, int NS, int ROWS>
 struct Inner {
   static constexpr bool F32 = sizeof(T) == 4;
   static constexpr int QUADS = NS * (Mma<T>::STEP / 4), ALL = ROWS * QUADS, EACH = (ALL + 255) / 256;
   static constexpr int ROW = NS * 64 + 16, PLANE = ROWS * ROW, BYTES = (F32 ? 1 : 2) * PLANE;      // in LDS (rows apart in the banks)
   floatx4 t[EACH];
+  static __device__ inline bool mine(const AdapterArgs& p, int q) { return q < ALL && q % QUADS < p.rank / 4; }
+  static __device__ inline const float* first_range(const AdapterArgs& p, int64_t m0, int rows_left, int part, int q) {
+    return reinterpret_cast<const float*>(p.workspace) + (m0 + min(q / QUADS, rows_left - 1)) * (p.parts * p.rank) + part * p.rank + 4 * (q % QUADS);
+  }
   __device__ inline void load(const AdapterArgs& p, int splits, int64_t m0, int rows_left, int part) {
-    const int inner = p.parts * p.rank;
-    const int64_t plane = (int64_t)p.M * inner;
+    const int64_t plane = (int64_t)p.M * p.parts * p.rank;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-      const int q = (int)threadIdx.x + 256 * i, row = min(q / QUADS, rows_left - 1), r = q % QUADS;
+      const int q = (int)threadIdx.x + 256 * i;
       t[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-      if (q >= ALL || r >= p.rank / 4) continue;
-      const float* from = reinterpret_cast<const float*>(p.workspace) + (m0 + row) * inner + part * p.rank + 4 * r;
+      if (!mine(p, q)) continue;
+      const float* from = first_range(p, m0, rows_left, part, q);
       constexpr int AT_ONCE = EACH > 2 ? 4 : 8;
       for (int z = 0; z < splits; z += AT_ONCE) {
         floatx4 v[AT_ONCE];
@@ -203,6 +213,45 @@ struct Inner {
         *reinterpret_cast<u32x2*>(to) = hi;
         *reinterpret_cast<u32x2*>(to + PLANE) = u32x2{pack_bf2(v[0] - bf_lo(hi[0]), v[1] - bf_hi(hi[0])), pack_bf2(v[2] - bf_lo(hi[1]), v[3] - bf_hi(hi[1]))};
       }
+    }
+  }
+};
+
+// The same in two: requested, and added up once what is requested next is under way (4096 x 4096, rank 64: 39.2 | 36.6 us for both launches; blocks of
+// 16 rows lose by it what the registers cost, 61 rows 15.5 | 16.4 us)
+template <typename T, int NS, int ROWS>
+struct InnerAhead : Inner<T, NS, ROWS> {
+  typedef Inner<T, NS, ROWS> I;
+  static constexpr int FIRST = I::EACH > 4 ? 1 : I::EACH == 4 && NS == 4 ? 2 : 4;      // ranges at once, as registers allow
+  floatx4 v[I::EACH][FIRST];
+  const float* from[I::EACH];
+  __device__ inline void ranges(const AdapterArgs& p, int splits, int z) {
+    const int64_t plane = (int64_t)p.M * p.parts * p.rank;
+#pragma unroll
+    for (int k = 0; k < FIRST; ++k)
+      if (z + k < splits) {
+#pragma unroll
+        for (int i = 0; i < I::EACH; ++i)
+          if (I::mine(p, (int)threadIdx.x + 256 * i)) v[i][k] = *reinterpret_cast<const floatx4*>(from[i] + (z + k) * plane);
+      }
+  }
+  __device__ inline void request(const AdapterArgs& p, int splits, int64_t m0, int part) {
+#pragma unroll
+    for (int i = 0; i < I::EACH; ++i) from[i] = I::first_range(p, m0, ROWS, part, (int)threadIdx.x + 256 * i);
+    ranges(p, splits, 0);
+  }
+  __device__ inline void sum(const AdapterArgs& p, int splits) {
+#pragma unroll
+    for (int i = 0; i < I::EACH; ++i) this->t[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int z = 0; z < splits; z += FIRST) {
+      if (z > 0) ranges(p, splits, z);
+#pragma unroll
+      for (int k = 0; k < FIRST; ++k)
+        if (z + k < splits) {
+#pragma unroll
+          for (int i = 0; i < I::EACH; ++i)
+            if (I::mine(p, (int)threadIdx.x + 256 * i)) this->t[i] += v[i][k];
+        }
     }
   }
 };
@@ -255,8 +304,7 @@ __device__ inline void products(floatx4 (&acc)[4], const u32x4 (&bf)[4][NS], con
   }
 }
 
-// y of 16 rows from m0 on and columns b0 .. b1 - 1, 64 a wave at a time; of the rows' adapters every `lanes`-th from `lane0` on.  t0: t of the part that
-// b0 belongs to, requested before the adapters are known.
+// y of 16 rows from m0 on and columns b0 .. b1 - 1, 64 a wave at a time; of the rows' adapters every `lanes`-th from `lane0` on
 template <typename T, int NS>
 __device__ inline void outer_rows(const AdapterArgs& p, const Cut& cut, int lanes, int lane0, int64_t m0, int b0, int b1, char* tl) {
   typedef typename Four<T>::type F;
@@ -269,7 +317,7 @@ __device__ inline void outer_rows(const AdapterArgs& p, const Cut& cut, int lane
   I t;
   t.load(p, cut.splits, m0, rows_left, part0);
   int have = part0;
-  const Rows rows(p, m0, 16);
+  const Rows rows(p, Rows::request(p, m0, 16));
   const T* const base = reinterpret_cast<const T*>(p.base) + m0 * p.ldy;
   T* const y = reinterpret_cast<T*>(p.y) + m0 * p.ldy;
   const bool wide = p.ldy % 4 == 0;        // rows at addresses for wide accesses
@@ -337,43 +385,39 @@ __global__ __launch_bounds__(256, 2) void adapters_outer_kernel(AdapterArgs p, C
   __shared__ __attribute__((aligned(16))) char tl[Inner<T, NS, 16>::BYTES];
   const int cols = 64 * cut.groups, chunks = ceil_div(p.N, cols);
   const int b0 = blockIdx.x % chunks * cols;
-  outer_rows<T, NS>(p, cut, cut.lanes, blockIdx.y, (int64_t)(blockIdx.x / chunks) * 16, b0, min(b0 + cols, p.N), tl);
+  outer_rows<T, NS>(p, cut, cut.lanes, blockIdx.y, (int64_t)(cut.first + (int)(blockIdx.x / chunks)) * 16, b0, min(b0 + cols, p.N), tl);
 }
 
-// Many rows: 64 of them and 256 columns of one part, 64 a wave.  Most share an adapter: base, b and t are requested at once and no row is tested (beside memory,
-// instructions bound these blocks), and a row's accesses are one offset a lane from scalar addresses, past the caches (4096 x 4096, rank 64: 24.0 | 20.4 us).
-// Where they do not, one adapter after another.
+// Many rows: 64 of them and 256 columns of one part, all there, 64 columns a wave.  Most share an adapter: base, b and t are requested at once and no
+// row is tested (beside memory, instructions bound these blocks), and a row's accesses are one offset a lane from one address a row, past the caches
+// (4096 x 4096, rank 64: 24.0 | 20.4 us).  Where they do not, one adapter after another.
 template <typename T, int NS>
 __global__ __launch_bounds__(256, 2) void adapters_outer_many_kernel(AdapterArgs p, Cut cut) {
   typedef typename Four<T>::type F;
-  typedef Inner<T, NS, 64> I;
+  typedef InnerAhead<T, NS, 64> I;
   __shared__ __attribute__((aligned(16))) char tl[I::BYTES];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, kg = lane >> 4;
-  const int chunks = ceil_div(p.N, 256);
+  const int chunks = p.N / 256;
   const int turn = blockIdx.x / 8;         // of the XCDs: each works on whole rows
   const int64_t m0 = (int64_t)(turn / chunks * 8 + blockIdx.x % 8) * 64;
-  if (m0 >= p.M) return;
-  const int b0 = turn % chunks * 256, b1 = min(b0 + 256, p.N);
+  if (m0 + 64 > p.M) return;
+  const int b0 = turn % chunks * 256;
   int part = 0;
   while (b0 >= p.part_end[part]) ++part;
-  if (m0 + 64 > p.M || b1 - b0 != 256 || b1 > p.part_end[part] || p.ldy % 4 != 0) {
-#pragma unroll 1
-    for (int i = 0; i < 4 && m0 + 16 * i < p.M; ++i) outer_rows<T, NS>(p, cut, 1, 0, m0 + 16 * i, b0, b1, tl);
-    return;
-  }
   const int n0 = b0 + 64 * wave;
   const int64_t row = p.ldy * (int64_t)sizeof(T);
   const uint32_t at = 4 * kg * (uint32_t)row + 4 * c * (uint32_t)sizeof(T);      // (ldy is at most 2^24)
   const char* const base = reinterpret_cast<const char*>(p.base) + m0 * row + n0 * (int64_t)sizeof(T);
   char* const y = reinterpret_cast<char*>(p.y) + m0 * row + n0 * (int64_t)sizeof(T);
+  const int ids = Rows::request(p, m0, 64);
   F old[4][4];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int e = 0; e < 4; ++e) old[i][e] = __builtin_nontemporal_load(reinterpret_cast<const F*>(base + (16 * i + e) * row + at));
   I t;
-  t.load(p, cut.splits, m0, 64, part);
-  const Rows rows(p, m0, 64);
+  t.request(p, cut.splits, m0, part);
+  const Rows rows(p, ids);
   const uint64_t none = __ballot(rows.id < 0);
   int id = __builtin_amdgcn_readlane(rows.id, rows.leaders != 0 ? __ffsll((unsigned long long)rows.leaders) - 1 : 0);
   u32x4 bf[4][NS];
@@ -386,6 +430,7 @@ __global__ __launch_bounds__(256, 2) void adapters_outer_many_kernel(AdapterArgs
         if (none >> (16 * i + 4 * kg + e) & 1) *reinterpret_cast<F*>(y + (16 * i + e) * row + at) = old[i][e];
   }
   if (rows.leaders == 0) return;
+  t.sum(p, cut.splits);
   t.store(tl, [&](int r) {
     const int whose = __shfl(rows.id, r, 64);
     return p.scale != nullptr ? p.scale[max(whose, 0)] : 1.f;
@@ -420,6 +465,13 @@ __global__ __launch_bounds__(256, 2) void adapters_outer_many_kernel(AdapterArgs
 // From here on the blocks take 64 rows: most of them share an adapter with their neighbours
 constexpr int MANY = 1024;
 
+// Blocks beside one another that deal a tile's adapters, of which 16 rows have at most 16, where there are few tiles
+int lanes_of(int64_t blocks, int rows) {
+  const int64_t l = ceil_div64(8 * compute_units(), blocks);
+  const int most = rows < 16 ? rows : 16;
+  return (int)(l < 1 ? 1 : l < most ? l : most);
+}
+
 // K in ranges until the blocks fill the chip twice (of many rows once: 4096 x 4096, rank 64, 4 | 8 ranges 15.2 | 15.6 us, and less to add up)
 Cut cut_of(int M, int K, int inner, forge_dtype dt) {
   const int units = ceil_div(K, dt == FORGE_BF16 ? 256 : 128);
@@ -431,39 +483,49 @@ Cut cut_of(int M, int K, int inner, forge_dtype dt) {
   const int most = M >= MANY ? units : ceil_div(units, 2);     // (two units a block: both are on their way at once)
   c.splits = want < most ? want : most;
   c.lanes = c.groups = 1;
+  c.first = 0;
   return c;
 }
 
+// whether the columns are whole blocks of the second launch for many rows
+bool whole_blocks(const AdapterArgs& a) {
+  bool whole = a.ldy % 4 == 0;
+  for (int i = 0; i < a.parts; ++i) whole = whole && a.part_end[i] % 256 == 0;
+  return whole;
+}
+
 template <typename T, int NS>
-void launch_outer(const AdapterArgs& a, const Cut& c, const dim3& grid, hipStream_t s) {
-  if (a.M >= MANY) adapters_outer_many_kernel<T, NS><<<grid, 256, 0, s>>>(a, c);
-  else adapters_outer_kernel<T, NS><<<grid, 256, 0, s>>>(a, c);
+forge_status launch_outer(const AdapterArgs& a, Cut c, hipStream_t s) {
+  if (a.M >= MANY && whole_blocks(a)) {
+    adapters_outer_many_kernel<T, NS><<<(unsigned)(ceil_div(a.M / 64, 8) * 8 * (a.N / 256)), 256, 0, s>>>(a, c);
+    if (a.M % 64 == 0) return launch_status();
+    if (hipGetLastError() != hipSuccess) return FORGE_ERR_HIP;
+    c.first = a.M / 64 * 4;
+  }
+  const int rows = a.M - 16 * c.first;
+  c.groups = a.N <= 256 ? 4 : 8;
+  const int64_t blocks = (int64_t)ceil_div(rows, 16) * ceil_div(a.N, 64 * c.groups);
+  c.lanes = lanes_of(blocks, rows);
+  adapters_outer_kernel<T, NS><<<dim3((unsigned)blocks, c.lanes), 256, 0, s>>>(a, c);
+  return launch_status();
 }
 template <typename T>
 forge_status launch(const AdapterArgs& a, hipStream_t s) {
-  const int cus = compute_units(), inner = a.parts * a.rank;
+  const int inner = a.parts * a.rank;
   const bool many = a.M >= MANY;
   Cut c = cut_of(a.M, a.K, inner, a.dt);
-  auto lanes = [&](int64_t blocks) {                           // a tile of 16 rows has at most 16 adapters
-    const int64_t l = ceil_div64(8 * cus, blocks);
-    const int most = many ? 1 : a.M < 16 ? a.M : 16;
-    return (int)(l < 1 ? 1 : l < most ? l : most);
-  };
-  c.lanes = many ? 2 : lanes((int64_t)c.tiles * c.chunks * c.splits);
+  c.lanes = many ? 2 : lanes_of((int64_t)c.tiles * c.chunks * c.splits, a.M);
   const dim3 grid(c.tiles, c.chunks * c.splits, c.lanes);
   if (many) adapters_inner_kernel<T, 4><<<grid, 256, 0, s>>>(a, c);
   else adapters_inner_kernel<T, 1><<<grid, 256, 0, s>>>(a, c);
   if (hipGetLastError() != hipSuccess) return FORGE_ERR_HIP;
-  c.groups = many || a.N <= 256 ? 4 : 8;
-  const int64_t blocks = (int64_t)(many ? ceil_div(c.tiles, 8) * 8 : c.tiles) * ceil_div(a.N, 64 * c.groups);
-  c.lanes = lanes(blocks);
-  const dim3 outer((unsigned)blocks, c.lanes);
   const int steps = ceil_div(a.rank, Mma<T>::STEP);
-  if (steps == 1) launch_outer<T, 1>(a, c, outer, s);
-  else if (steps == 2) launch_outer<T, 2>(a, c, outer, s);
-  else if (steps <= 4) launch_outer<T, 4>(a, c, outer, s);
-  else if constexpr (sizeof(T) == 4) launch_outer<T, 8>(a, c, outer, s);
-  return launch_status();
+  if (steps == 1) return launch_outer<T, 1>(a, c, s);
+  if (steps == 2) return launch_outer<T, 2>(a, c, s);
+  if constexpr (sizeof(T) == 4) {
+    if (steps > 4) return launch_outer<T, 8>(a, c, s);
+  }
+  return launch_outer<T, 4>(a, c, s);
 }
 
 }  // namespace
