@@ -5,8 +5,8 @@
 // infinity of one request's adapter reaches another's rows).  Neighbours in a batch of requests have different adapters, so a tile's adapters are dealt
 // over blocks (`lanes`) where there are few tiles; the rows of a prompt share one, and blocks then take 64 of them.
 // An adapter is read once per tile that has it: with the chain adapter number, adapter, sum of each launch that bounds a decode step (61 rows, 49 adapters
-// of rank 16 beside q, k and v of 4096: 8 + 8.6 us for 19 + 10 MB of adapters).  The rows of x, base and y bound a prompt (4096 rows of 5 requests, rank 64,
-// 4096 x 4096: 16.6 + 23 us for 34 + 67 MB; one row of 768 in fp32 4.3 + 4.9).
+// of rank 16 beside q, k and v of 4096: 8 + 8 us for 19 + 10 MB of adapters).  The rows of x, base and y bound a prompt (4096 rows of 5 requests, rank 64,
+// 4096 x 4096: 15.8 + 21.3 us for 34 + 67 MB; one row of 768 in fp32 4.4 + 4.6).
 #include "paged.hpp"
 
 namespace forge {
