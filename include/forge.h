@@ -558,7 +558,8 @@ typedef struct {
 /* y[m, n] = base[m, n] + scale[i] * sum_r b[i, n, r] * (sum_k a[i, part(n) * rank + r, k] x[m, k]),  i = ids[m]
  * x: [M, K]; base, y: [M, N] with row stride ldy (0: N); base may be y, x must not be.  ids: DEVICE int32 [M]; rows whose id is outside [0, n_adapters)
  * get base alone (not touched where y is base).  For the output of a projection without an activation, int8 or not: y = base = that output.
- * fp32 sums, also of the first product (bf16: as two bf16 parts in the second), one rounding to dt.  Rows of a request next to one another share the reads
+ * fp32 sums, also of the first product (bf16: as two bf16 parts in the second, so that an infinity in b gives an infinity or NaN), one rounding to dt.
+ * What is not finite stays in its own row and, in an adapter, in the rows that use it.  Rows of a request next to one another share the reads
  * of its adapter.  The workspace is required where its size is not 0; the size for M serves every smaller one. */
 size_t forge_adapters_workspace_bytes(const forge_adapters* adapters, int M);
 forge_status forge_adapters_add(const forge_adapters* adapters, const void* x, const void* base, void* y, const int32_t* ids,

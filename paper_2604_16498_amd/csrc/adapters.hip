@@ -211,7 +211,10 @@ struct Inner {
       else {
         const u32x2 hi = {pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3])};
         *reinterpret_cast<u32x2*>(to) = hi;
-        *reinterpret_cast<u32x2*>(to + PLANE) = u32x2{pack_bf2(v[0] - bf_lo(hi[0]), v[1] - bf_hi(hi[0])), pack_bf2(v[2] - bf_lo(hi[1]), v[3] - bf_hi(hi[1]))};
+        // (an infinity has no second part: it would take it back)
+        auto rest = [](float v, float hi) { return fabsf(hi) < INFINITY ? v - hi : 0.f; };
+        *reinterpret_cast<u32x2*>(to + PLANE) = u32x2{pack_bf2(rest(v[0], bf_lo(hi[0])), rest(v[1], bf_hi(hi[0]))),
+                                                      pack_bf2(rest(v[2], bf_lo(hi[1])), rest(v[3], bf_hi(hi[1])))};
       }
     }
   }

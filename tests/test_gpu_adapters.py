@@ -108,6 +108,24 @@ def test_infinities_reach_the_rows_of_their_adapter_alone(M):
     assert torch.isnan(dirty[~rows][:, 100]).all() and not torch.isfinite(dirty[~rows]).any()
 
 
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("M", [9, 1100])
+def test_an_infinite_input_stays_infinite(M, bf16):
+    """positive adapters: x = inf gives inf, -inf in another row -inf, not NaN"""
+    rng = np.random.default_rng(M)
+    dt = torch.bfloat16 if bf16 else torch.float32
+    x, base, a, b = (gpu(z, dt) for z in (normal(rng, (M, 64)), normal(rng, (M, 320)), np.abs(normal(rng, (2, 16, 64))) + 0.1, np.abs(normal(rng, (2, 320, 16))) + 0.1))
+    ids = [m % 2 for m in range(M)]
+    d = F.make_adapters(a, b)
+    call = lambda: F.forge_adapters_add(d, x, base, torch.empty_like(base), ints(ids), workspace=F.workspace(F.forge_adapters_workspace_bytes(d, M)))
+    clean = call()
+    x[3, 11], x[M - 1, 60] = float("inf"), -float("inf")
+    got = call()
+    assert (got[3] == float("inf")).all() and (got[M - 1] == -float("inf")).all()
+    rest = [m for m in range(M) if m not in (3, M - 1)]
+    assert torch.equal(got[rest], clean[rest])
+
+
 def test_offsets_past_32_bits():
     """adapters more than 2^32 bytes into their tensors"""
     rng = np.random.default_rng(3)
