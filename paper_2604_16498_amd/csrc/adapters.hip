@@ -52,8 +52,8 @@ struct Rows {
   }
 };
 
-// groups: of 64 columns, a block of the second launch; first: tile of 16 rows that it begins with
-struct Cut { int tiles, splits, chunks, lanes, groups, first; };
+// groups: of 64 columns, a block of the second launch
+struct Cut { int tiles, splits, chunks, lanes, groups; };
 
 // t of 16 RT rows and 64 inner columns over one range of K, in units of 512 bytes a row: a load of a block is 8 rows x 512 bytes (a kernel that only
 // read 4096 rows of 8 KB took 7.9 us so, 12.0 in lines of 128 bytes), two units of x and of the adapter are on their way in registers, and a unit
@@ -388,7 +388,7 @@ __global__ __launch_bounds__(256, 2) void adapters_outer_kernel(AdapterArgs p, C
   __shared__ __attribute__((aligned(16))) char tl[Inner<T, NS, 16>::BYTES];
   const int cols = 64 * cut.groups, chunks = ceil_div(p.N, cols);
   const int b0 = blockIdx.x % chunks * cols;
-  outer_rows<T, NS>(p, cut, cut.lanes, blockIdx.y, (int64_t)(cut.first + (int)(blockIdx.x / chunks)) * 16, b0, min(b0 + cols, p.N), tl);
+  outer_rows<T, NS>(p, cut, cut.lanes, blockIdx.y, (int64_t)(blockIdx.x / chunks) * 16, b0, min(b0 + cols, p.N), tl);
 }
 
 // Many rows: 64 of them and 256 columns of one part, all there, 64 columns a wave.  Most share an adapter: base, b and t are requested at once and no
@@ -402,8 +402,10 @@ __global__ __launch_bounds__(256, 2) void adapters_outer_many_kernel(AdapterArgs
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, kg = lane >> 4;
   const int chunks = p.N / 256;
   const int turn = blockIdx.x / 8;         // of the XCDs: each works on whole rows
-  const int64_t m0 = (int64_t)(turn / chunks * 8 + blockIdx.x % 8) * 64;
-  if (m0 + 64 > p.M) return;
+  const int tile0 = (turn / chunks * 8 + (int)blockIdx.x % 8) * 64;
+  if (tile0 >= p.M) return;
+  const int64_t m0 = min(tile0, p.M - 64);           // (the last one begins among the rows of the one before, which are not its own)
+  const uint64_t own = ~0ull << (tile0 - (int)m0);
   const int b0 = turn % chunks * 256;
   int part = 0;
   while (b0 >= p.part_end[part]) ++part;
@@ -420,8 +422,8 @@ __global__ __launch_bounds__(256, 2) void adapters_outer_many_kernel(AdapterArgs
     for (int e = 0; e < 4; ++e) old[i][e] = __builtin_nontemporal_load(reinterpret_cast<const F*>(base + (16 * i + e) * row + at));
   I t;
   t.request(p, cut.splits, m0, part);
-  const Rows rows(p, ids);
-  const uint64_t none = __ballot(rows.id < 0);
+  const Rows rows(p, own >> lane & 1 ? ids : -1);
+  const uint64_t none = __ballot(rows.id < 0) & own;
   int id = __builtin_amdgcn_readlane(rows.id, rows.leaders != 0 ? __ffsll((unsigned long long)rows.leaders) - 1 : 0);
   u32x4 bf[4][NS];
   if (rows.leaders != 0) load_b<T, NS>(bf, p, id, n0);
@@ -465,8 +467,15 @@ __global__ __launch_bounds__(256, 2) void adapters_outer_many_kernel(AdapterArgs
   }
 }
 
-// From here on the blocks take 64 rows: most of them share an adapter with their neighbours
-constexpr int MANY = 1024;
+// Whether blocks take 64 rows, most of which share an adapter with their neighbours: where there are enough tiles of 64 rows and 256 columns.  bf16, 64 rows |
+// 16, us: 768 x 768, rank 64, 768 rows (36 tiles) 13.5 | 12.3, 1000 (47) 13.6 | 13.6, 1500 14.2 | 14.9; 4096 x 4096, 300 rows (80) 18.1 | 17.0, 512 18.7 | 19.3,
+// 2048 26.9 | 31.5.  In fp32 matrix instructions take 8 times as long, and so the chain of a block: 768 x 768, rank 64, 2048 rows (96) 27.7 | 24.2,
+// 4096 33.7 | 34.0, 2304 columns of 4096 rows (576) 60.8 | 66.2; rank 8, 2304 columns of 1024 rows (144) 15.3 | 18.2.
+constexpr int MANY = 512;
+bool many_rows(int M, int N, int rank, forge_dtype dt) {
+  const int64_t tiles = (int64_t)(M / 64) * ceil_div(N, 256);
+  return M >= MANY && tiles >= (dt == FORGE_BF16 ? 44 : 128 * ceil_div(rank, Mma<float>::STEP));
+}
 
 // Blocks beside one another that deal a tile's adapters, of which 16 rows have at most 16, where there are few tiles
 int lanes_of(int64_t blocks, int rows) {
@@ -476,17 +485,16 @@ int lanes_of(int64_t blocks, int rows) {
 }
 
 // K in ranges until the blocks fill the chip twice (of many rows once: 4096 x 4096, rank 64, 4 | 8 ranges 15.2 | 15.6 us, and less to add up)
-Cut cut_of(int M, int K, int inner, forge_dtype dt) {
+Cut cut_of(int M, int K, int inner, bool many, forge_dtype dt) {
   const int units = ceil_div(K, dt == FORGE_BF16 ? 256 : 128);
   Cut c;
-  c.tiles = ceil_div(M, M >= MANY ? 64 : 16);
+  c.tiles = ceil_div(M, many ? 64 : 16);
   c.chunks = ceil_div(inner, 16 * JT);
   const int64_t blocks = (int64_t)c.tiles * c.chunks;
-  const int want = (int)ceil_div64((M >= MANY ? 1 : 2) * compute_units(), blocks);
-  const int most = M >= MANY ? units : ceil_div(units, 2);     // (two units a block: both are on their way at once)
+  const int want = (int)ceil_div64((many ? 1 : 2) * compute_units(), blocks);
+  const int most = many ? units : ceil_div(units, 2);     // (two units a block: both are on their way at once)
   c.splits = want < most ? want : most;
   c.lanes = c.groups = 1;
-  c.first = 0;
   return c;
 }
 
@@ -498,37 +506,34 @@ bool whole_blocks(const AdapterArgs& a) {
 }
 
 template <typename T, int NS>
-forge_status launch_outer(const AdapterArgs& a, Cut c, hipStream_t s) {
-  if (a.M >= MANY && whole_blocks(a)) {
-    adapters_outer_many_kernel<T, NS><<<(unsigned)(ceil_div(a.M / 64, 8) * 8 * (a.N / 256)), 256, 0, s>>>(a, c);
-    if (a.M % 64 == 0) return launch_status();
-    if (hipGetLastError() != hipSuccess) return FORGE_ERR_HIP;
-    c.first = a.M / 64 * 4;
+forge_status launch_outer(const AdapterArgs& a, Cut c, bool many, hipStream_t s) {
+  if (many && whole_blocks(a)) {
+    adapters_outer_many_kernel<T, NS><<<(unsigned)(ceil_div(ceil_div(a.M, 64), 8) * 8 * (a.N / 256)), 256, 0, s>>>(a, c);
+    return launch_status();
   }
-  const int rows = a.M - 16 * c.first;
   c.groups = a.N <= 256 ? 4 : 8;
-  const int64_t blocks = (int64_t)ceil_div(rows, 16) * ceil_div(a.N, 64 * c.groups);
-  c.lanes = lanes_of(blocks, rows);
+  const int64_t blocks = (int64_t)ceil_div(a.M, 16) * ceil_div(a.N, 64 * c.groups);
+  c.lanes = lanes_of(blocks, a.M);
   adapters_outer_kernel<T, NS><<<dim3((unsigned)blocks, c.lanes), 256, 0, s>>>(a, c);
   return launch_status();
 }
 template <typename T>
 forge_status launch(const AdapterArgs& a, hipStream_t s) {
   const int inner = a.parts * a.rank;
-  const bool many = a.M >= MANY;
-  Cut c = cut_of(a.M, a.K, inner, a.dt);
+  const bool many = many_rows(a.M, a.N, a.rank, a.dt);
+  Cut c = cut_of(a.M, a.K, inner, many, a.dt);
   c.lanes = many ? 2 : lanes_of((int64_t)c.tiles * c.chunks * c.splits, a.M);
   const dim3 grid(c.tiles, c.chunks * c.splits, c.lanes);
   if (many) adapters_inner_kernel<T, 4><<<grid, 256, 0, s>>>(a, c);
   else adapters_inner_kernel<T, 1><<<grid, 256, 0, s>>>(a, c);
   if (hipGetLastError() != hipSuccess) return FORGE_ERR_HIP;
   const int steps = ceil_div(a.rank, Mma<T>::STEP);
-  if (steps == 1) return launch_outer<T, 1>(a, c, s);
-  if (steps == 2) return launch_outer<T, 2>(a, c, s);
+  if (steps == 1) return launch_outer<T, 1>(a, c, many, s);
+  if (steps == 2) return launch_outer<T, 2>(a, c, many, s);
   if constexpr (sizeof(T) == 4) {
-    if (steps > 4) return launch_outer<T, 8>(a, c, s);
+    if (steps > 4) return launch_outer<T, 8>(a, c, many, s);
   }
-  return launch_outer<T, 4>(a, c, s);
+  return launch_outer<T, 4>(a, c, many, s);
 }
 
 }  // namespace

@@ -70,6 +70,25 @@ def test_adapters_of_prompts(M, K, ends, rank, requests, bf16):
     check(rng, M, K, ends, rank, 6, runs(rng, M, 6, requests), bf16)
 
 
+# whole blocks of columns and rows that end inside a tile, in place and not, in the larger tiles and next to where they begin
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("M,K,ends,rank,requests", [
+    (511, 72, [1536], 16, 4), (512, 72, [1536], 16, 4), (577, 264, [512, 1536], 64, 200), (703, 64, [1024], 8, 5), (704, 64, [1024], 8, 5),
+    (1025, 136, [1024], 16, 1), (1090, 72, [256, 768, 2048], 16, 400), (1100, 64, [4096], 24, 3), (2050, 64, [4096], 64, 9)])
+def test_adapters_of_prompts_beside_whole_blocks(M, K, ends, rank, requests, bf16):
+    rng = np.random.default_rng(M + K)
+    ids = runs(rng, M, 6, requests)
+    check(rng, M, K, ends, rank, 6, ids, bf16)
+    check(rng, M, K, ends, rank, 6, ids, bf16, in_place=True)
+    check(rng, M, K, ends, rank, 6, ids, bf16, ldy=ends[-1] + 8, in_place=True, scaled=False)
+
+
+@pytest.mark.parametrize("bf16,rank", [(True, 128), (False, 72)])
+def test_large_ranks_of_prompts(bf16, rank):
+    rng = np.random.default_rng(rank)
+    check(rng, 2570, 64, [4096], rank, 6, runs(rng, 2570, 6, 9), bf16, in_place=True)
+
+
 @pytest.mark.parametrize("bf16", [True, False])
 @pytest.mark.parametrize("M", [3, 40, 1030])
 def test_in_place_strides_and_odd_addresses(M, bf16):
