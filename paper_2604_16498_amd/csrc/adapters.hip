@@ -467,19 +467,22 @@ __global__ __launch_bounds__(256, 2) void adapters_outer_many_kernel(AdapterArgs
   }
 }
 
-// Whether blocks take 64 rows, most of which share an adapter with their neighbours: where there are enough tiles of 64 rows and 256 columns.  bf16, 64 rows |
-// 16, us: 768 x 768, rank 64, 768 rows (36 tiles) 13.5 | 12.3, 1000 (47) 13.6 | 13.6, 1500 14.2 | 14.9; 4096 x 4096, 300 rows (80) 18.1 | 17.0, 512 18.7 | 19.3,
-// 2048 26.9 | 31.5.  In fp32 matrix instructions take 8 times as long, and so the chain of a block: 768 x 768, rank 64, 2048 rows (96) 27.7 | 24.2,
-// 4096 33.7 | 34.0, 2304 columns of 4096 rows (576) 60.8 | 66.2; rank 8, 2304 columns of 1024 rows (144) 15.3 | 18.2.
+// Whether blocks take 64 rows, most of which share an adapter with their neighbours: where their tiles of 64 rows and 256 columns, and in the first launch
+// 64 rows and 64 inner columns, are enough.  bf16, 64 rows | 16, us: 768 x 768, rank 64, 1500 rows (69 tiles) 14.2 | 14.0, 4096 (192) 15.5 | 18.7; 4096 x 4096,
+// rank 64, 512 rows (128, 8 in the first launch) 18.6 | 17.0, 1000 20.9 | 22.4, 4096 36.6 | 50.4; beside q, k and v (192, 24) 24.5 | 28.0.  In fp32 a block's
+// chain of matrix instructions is 8 times as long: 2304 x 768, rank 64, 1500 rows (207 tiles) 36.1 | 35.6, 4096 (576) 61.5 | 71.1; rank 8 17.9 | 16.3 and
+// 30.1 | 31.4.
 constexpr int MANY = 512;
-bool many_rows(int M, int N, int rank, forge_dtype dt) {
+bool many_rows(int M, int N, int inner, forge_dtype dt) {
   const int64_t tiles = (int64_t)(M / 64) * ceil_div(N, 256);
-  return M >= MANY && tiles >= (dt == FORGE_BF16 ? 44 : 128 * ceil_div(rank, Mma<float>::STEP));
+  return M >= MANY && (int64_t)M * ceil_div(inner, 16 * JT) >= 900 && tiles >= (dt == FORGE_BF16 ? 72 : 256);
 }
 
-// Blocks beside one another that deal a tile's adapters, of which 16 rows have at most 16, where there are few tiles
+// Blocks beside one another that deal a tile's adapters, of which 16 rows have at most 16, where there are few tiles: as many as are resident at once (a
+// tile of a prompt has one adapter, and what more there are pass over it in turn; 3 | 8 per CU in both launches, 4096 x 4096, us: 500 rows of 5 requests,
+// rank 64, 16.9 | 19.6; 256 requests of rank 8 20.0 | 26.1)
 int lanes_of(int64_t blocks, int rows) {
-  const int64_t l = ceil_div64(8 * compute_units(), blocks);
+  const int64_t l = ceil_div64(3 * compute_units(), blocks);
   const int most = rows < 16 ? rows : 16;
   return (int)(l < 1 ? 1 : l < most ? l : most);
 }
@@ -520,7 +523,7 @@ forge_status launch_outer(const AdapterArgs& a, Cut c, bool many, hipStream_t s)
 template <typename T>
 forge_status launch(const AdapterArgs& a, hipStream_t s) {
   const int inner = a.parts * a.rank;
-  const bool many = many_rows(a.M, a.N, a.rank, a.dt);
+  const bool many = many_rows(a.M, a.N, inner, a.dt);
   Cut c = cut_of(a.M, a.K, inner, many, a.dt);
   c.lanes = many ? 2 : lanes_of((int64_t)c.tiles * c.chunks * c.splits, a.M);
   const dim3 grid(c.tiles, c.chunks * c.splits, c.lanes);

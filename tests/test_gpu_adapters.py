@@ -74,7 +74,7 @@ def test_adapters_of_prompts(M, K, ends, rank, requests, bf16):
 @pytest.mark.parametrize("bf16", [True, False])
 @pytest.mark.parametrize("M,K,ends,rank,requests", [
     (511, 72, [1536], 16, 4), (512, 72, [1536], 16, 4), (577, 264, [512, 1536], 64, 200), (703, 64, [1024], 8, 5), (704, 64, [1024], 8, 5),
-    (1025, 136, [1024], 16, 1), (1090, 72, [256, 768, 2048], 16, 400), (1100, 64, [4096], 24, 3), (2050, 64, [4096], 64, 9)])
+    (513, 72, [1024, 2048, 2304], 64, 40), (899, 64, [2048], 8, 3), (900, 64, [2048], 8, 3), (1100, 64, [4096], 16, 300), (1025, 136, [2048], 16, 1), (1090, 72, [256, 768, 2048], 16, 400), (1100, 64, [4096], 24, 3), (2050, 64, [4096], 64, 9)])
 def test_adapters_of_prompts_beside_whole_blocks(M, K, ends, rank, requests, bf16):
     rng = np.random.default_rng(M + K)
     ids = runs(rng, M, 6, requests)
