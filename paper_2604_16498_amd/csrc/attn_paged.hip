@@ -68,7 +68,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 && (S != FORGE_KV_SAME || D
   const int c = lane & 15, kg = lane >> 4;
   const bool twice = !F32 && p.rows <= 8;
   const int column = twice ? c & 7 : c;                        // the query head of this lane, counted in its block
-  const float rest = twice && c >= 8 ? 1.f : 0.f;
+  const uint32_t second = twice && c >= 8 ? ~0u : 0u;          // this lane's column holds what the weights lose
   char* const lds = patch[wave];
   const int in_page = (1 << p.shift) - 1;
 
@@ -227,8 +227,8 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 && (S != FORGE_KV_SAME || D
       u32x4 w;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const uint32_t hi = pack_bf2(s[2 * e], s[2 * e + 1]);
-        w[e] = pack_bf2(__builtin_fmaf(bf_lo(hi), -rest, s[2 * e]), __builtin_fmaf(bf_hi(hi), -rest, s[2 * e + 1]));
+        const uint32_t hi = pack_bf2(s[2 * e], s[2 * e + 1]) & second;      // (masked: an infinite weight times 0 would be NaN)
+        w[e] = pack_bf2(s[2 * e] - bf_lo(hi), s[2 * e + 1] - bf_hi(hi));
       }
       const bf16x8 pf = __builtin_bit_cast(bf16x8, w);
 #pragma unroll
