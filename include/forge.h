@@ -533,7 +533,8 @@ forge_status forge_paged_read(const forge_paged_cache* cache, int layer, const f
  * lengths: DEVICE int32 [batch], clamped to [0, max_len]; a request of length 0 (an idle place) gets zeros.  max_len: HOST, 1 ..
  * table_cols * page_rows and at most 2^30, sizes the launch and the workspace.  table: DEVICE int32 [batch, table_cols]; entries are clamped to
  * [0, n_pages), so that a bad one gives a wrong result for that request, never an access outside the pool; those past a request's last
- * row are not used.  What lies in rows behind a length, infinities and NaN among it, does not reach the output.
+ * row are not used.  What lies in rows behind a length, infinities and NaN among it, does not reach the output; an infinity in a row of v
+ * before it does, however small the row's weight (of a finite score; it is positive).
  * q: [batch, head, head_dim] view (its token_stride is not looked at); out: [batch, q_heads * head_dim] dense, in dt.  fp32 scores, statistics and
  * sums; for bf16 the weights are rounded to bf16 for the second product.  q_heads a multiple of kv_heads; (batch * kv_heads + 8) times the sixteens of
  * q_heads / kv_heads stay below 2^24.  The workspace size serves every smaller max_len and batch too. */

@@ -6,6 +6,8 @@
 // its range of rows in turn; the tile layouts, the products and the dealing of rows over blocks are those of the attention of drafted trees.
 // Up to 8 query heads a cache head: the 16 columns hold each twice, and the second takes what the weights of the first lose in bf16, so that they count with
 // 16 bits, for no further product (from 9 heads on they are rounded to bf16, 2^-9 each, as there).
+// A weight is positive, however far its row lies below the maximum: an infinity in that row of v counts.  So weights, the running rescaling and the
+// waves' and shares' parts do not become 0 where fp32 would round them to it; what that adds to a finite sum is 2^-133 of its rows of v.
 // What is its own is where a tile lies: in two halves of 16 rows, each inside a page, whose numbers a wave keeps in a
 // register, an entry a lane, for its next 32 tiles; a half's address is then scalar arithmetic.  A row is read once and goes past the caches.
 // Measured, 32 heads over 8 of 128: 64 requests up to 2049 rows, int8 (164 MB) 33.6 us, 4.9 TB/s (rows through the caches 37.0), two blocks a CU of uneven
@@ -16,6 +18,8 @@
 
 namespace forge {
 namespace {
+
+constexpr float LEAST = 9.183549615799121e-41f;      // 2^-133, the smallest positive number in bf16
 
 struct PagedParams {
   CacheView c;             // bs: of a page
@@ -122,6 +126,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 && (S != FORGE_KV_SAME || D
   };
   const int piece_row = lane / (L::ROW / 16), piece_at = lane % (L::ROW / 16) * 16;
   const int k_put = L::k_slot(piece_row) * L::STRIDE + piece_at, v_put = TILE * L::STRIDE + piece_row * L::STRIDE + piece_at;
+  bool odd_scale = false;                  // a row of the tile has a scale of v that is not finite
   // behind: rows from this one of the tile on are not the request's: their weights are 0, and their V is cleared (0 * infinity would be NaN)
   auto put_tile = [&](int behind) {
     wave_lds_sync();                       // the tile before has been read
@@ -136,7 +141,10 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 && (S != FORGE_KV_SAME || D
       *reinterpret_cast<u32x4*>(lds + k_put + L::k_slot(i * L::PER) * L::STRIDE) = rk[i];
 #pragma unroll
     for (int i = 0; i < L::LOADS; ++i) *reinterpret_cast<u32x4*>(lds + v_put + i * L::PER * L::STRIDE) = rv[i];
-    if constexpr (SCALED) *reinterpret_cast<float*>(lds + L::SCALES + lane * 4) = rs;
+    if constexpr (SCALED) {
+      *reinterpret_cast<float*>(lds + L::SCALES + lane * 4) = rs;
+      odd_scale = __any(lane >= TILE && !(fabsf(rs) < INFINITY));
+    }
     wave_lds_sync();
   };
   request(share.b, share.g, share.unit * UNIT);
@@ -198,18 +206,30 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 && (S != FORGE_KV_SAME || D
     for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[e]);
     if (__any(mx > m_run + 8.f)) {                       // (wave-uniform)
       const float m_new = fmaxf(m_run, lanes_max(mx));
-      const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+      const float alpha = share_weight(m_run - m_new);
       m_run = m_new;
       l_run *= alpha;
 #pragma unroll
       for (int m = 0; m < NM; ++m) acc[m] *= alpha;
     }
+    float w[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(s[e] - m_run);
+    bool tiny = odd_scale;                               // (8-bit rows have an infinity by their scale alone, one a lane)
+    if constexpr (!SCALED) {
+      uint32_t least = __float_as_uint(w[0]);            // (as integers they order like the values, NaN above all)
+#pragma unroll
+      for (int e = 1; e < 8; ++e) least = min(least, __float_as_uint(w[e]));
+      tiny = __any(least < 0x00800000u);
+    }
+    if (tiny) {                                          // (rare)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = s[e] > -INFINITY ? fmaxf(w[e], LEAST) : w[e];       // (NaN stays)
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float w = __builtin_amdgcn_exp2f(s[e] - m_run);
-      l_run += w;
-      s[e] = w;
-      if constexpr (SCALED) s[e] = w * vsr[e];
+      l_run += w[e];
+      s[e] = SCALED ? w[e] * vsr[e] : w[e];
     }
     if (SCALED && edge) {                                // (a row behind the length may have any scale)
 #pragma unroll
@@ -224,13 +244,13 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 && (S != FORGE_KV_SAME || D
 #pragma unroll
         for (int m = 0; m < NM; ++m) acc[m] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(r.v[e][m]), s[e], acc[m], 0, 0, 0);
     } else {
-      u32x4 w;
+      u32x4 words;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const uint32_t hi = pack_bf2(s[2 * e], s[2 * e + 1]) & second;      // (masked: an infinite weight times 0 would be NaN)
-        w[e] = pack_bf2(s[2 * e] - bf_lo(hi), s[2 * e + 1] - bf_hi(hi));
+        words[e] = pack_bf2(s[2 * e] - bf_lo(hi), s[2 * e + 1] - bf_hi(hi));
       }
-      const bf16x8 pf = __builtin_bit_cast(bf16x8, w);
+      const bf16x8 pf = __builtin_bit_cast(bf16x8, words);
 #pragma unroll
       for (int m = 0; m < NM; ++m)
         acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, St::v(r, m)), pf, acc[m], 0, 0, 0);
@@ -268,7 +288,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 && (S != FORGE_KV_SAME || D
     float lt = 0.f;
 #pragma unroll
     for (int w = w0; w < w0 + SIDE; ++w) {
-      const float a = __builtin_amdgcn_exp2f(sml[w][r][0] - mn);
+      const float a = share_weight(sml[w][r][0] - mn);
       floatx4 x = *reinterpret_cast<const floatx4*>(patch[w] + r * (PAD * 4) + d * 4);
       if (twice) {                         // (where a row has an infinity, the first part says which)
         const floatx4 y = *reinterpret_cast<const floatx4*>(patch[w] + (r + 8) * (PAD * 4) + d * 4);
