@@ -194,11 +194,12 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _stream():
+def _stream(d: Optional[int] = None):
+    """The current stream of the current device, which is d where the caller has asked for it already."""
     if _raw_stream is None:
         return C.c_void_p(torch.cuda.current_stream().cuda_stream)
     # the same handle without the Stream object around it (2.8 -> 0.2 us a call)
-    return _raw_stream(_device())
+    return _raw_stream(_device() if d is None else d)
 
 
 def _ws(t: Optional[torch.Tensor]):
@@ -511,7 +512,7 @@ def make_rope_desc(increments: torch.Tensor, style="half", factor=1.0) -> RopeDe
     if increments.dtype != torch.int64 or not increments.is_cuda or not increments.is_contiguous():
         raise ValueError("increments must be a contiguous int64 GPU tensor")
     r = RopeDesc(2 * increments.numel(), ROPE_STYLE[style], factor, increments.data_ptr())
-    r._increments = increments
+    r._increments, r._gpu = increments, increments.get_device()
     return r
 
 
@@ -656,37 +657,63 @@ def make_page_pool(free_pages, free_count, table, page_rows) -> PagePool:
         raise ValueError("free_pages must be [n_pages], table [batch, cols]")
     p = PagePool(free_pages.shape[0], page_rows, table.shape[0], table.shape[1], _int32(free_pages, free_pages.shape, "free_pages"),
                  _int32(free_count, (1,), "free_count"), _int32(table, table.shape, "table"))
-    p._tensors = (free_pages, free_count, table)
-    return p
+    return _keeping(p, (free_pages, free_count, table))
 
 
-def _here(t: torch.Tensor):
-    """The work goes to the current device's stream: its tensors have to lie there."""
-    if t.get_device() != _device():
-        raise ValueError("the tensors are on GPU %d, the current one is %d" % (t.get_device(), _device()))
+def _keeping(desc, tensors):
+    """A descriptor keeps its tensors alive, and the GPU that they lie on."""
+    desc._tensors, desc._gpu = tensors, tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != desc._gpu:
+            raise ValueError("a descriptor's tensors are on GPU %d and GPU %d" % (desc._gpu, t.get_device()))
+    return desc
 
 
-def _vector(t: torch.Tensor, n: int, what: str):
-    if t.dtype is not _INT32 or t.numel() != n or not t.is_cuda or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous int32 GPU tensor of %d entries" % (what, n))
+# The work goes to the current device's (d) stream: a call's tensors have to lie there, and its descriptors' (one filled in by hand does not
+# say where).  A device that is not d is a tensor on the CPU, too (-1), so that this one question is the only one.
+
+
+def _refuse(gpu: int, d: int, otherwise: str):
+    raise ValueError("a tensor of the call is on GPU %d, the current one is %d" % (gpu, d) if gpu not in (d, -1) else otherwise)
+
+
+def _here(desc, d: int):
+    gpu = getattr(desc, "_gpu", d)
+    if gpu != d:
+        _refuse(gpu, d, "a descriptor of tensors on the CPU")
+
+
+def _vector(t: torch.Tensor, n: int, what: str, d: int):
+    if t.get_device() != d or t.dtype is not _INT32 or t.numel() != n or not t.is_contiguous():
+        _refuse(t.get_device(), d, "%s must be a contiguous int32 GPU tensor of %d entries" % (what, n))
     return t.data_ptr()
+
+
+def _at(t: torch.Tensor, d: int):
+    if t.get_device() != d or not t.is_contiguous():
+        _refuse(t.get_device(), d, "forge tensors must be contiguous GPU tensors")
+    return t.data_ptr()
+
+
+def _ws_at(t: Optional[torch.Tensor], d: int):
+    return (None, 0) if t is None else (_at(t, d), t.nbytes)
 
 
 def forge_pages_assign(pool: PagePool, lengths, change, lengths_out, granted, starts, slots=None, positions=None, owners=None):
     """Lengths change by change[b] (int32 [batch]), pages move, and every new token gets slots, positions and owners (int32
     [max_tokens], or all None); granted [batch]: the changes that took place; starts [batch + 1]: the tokens of every request."""
-    B = pool.batch
-    _here(lengths)
+    B, d = pool.batch, _device()
+    _here(pool, d)
     if slots is None:
         if positions is not None or owners is not None:
             raise ValueError("slots, positions and owners come together")
         T, sp, pp, op = 0, None, None, None
     else:
         T = slots.numel()
-        sp, pp, op = _vector(slots, T, "slots"), _vector(positions, T, "positions"), _vector(owners, T, "owners")
-    _check(lib().forge_pages_assign(C.byref(pool), _vector(lengths, B, "lengths"), _vector(change, B, "change"),
-                                    _vector(lengths_out, B, "lengths_out"), _vector(granted, B, "granted"),
-                                    _vector(starts, B + 1, "starts"), sp, pp, op, T, _stream()), "forge_pages_assign")
+        sp, pp, op = _vector(slots, T, "slots", d), _vector(positions, T, "positions", d), _vector(owners, T, "owners", d)
+    _check(lib().forge_pages_assign(C.byref(pool), _vector(lengths, B, "lengths", d), _vector(change, B, "change", d),
+                                    _vector(lengths_out, B, "lengths_out", d), _vector(granted, B, "granted", d),
+                                    _vector(starts, B + 1, "starts", d), sp, pp, op, T, _stream(d)), "forge_pages_assign")
 
 
 def make_paged_cache(k, v, k_scale=None, v_scale=None) -> PagedCache:
@@ -697,23 +724,20 @@ def make_paged_cache(k, v, k_scale=None, v_scale=None) -> PagedCache:
                                flat.batch_stride, flat.head_stride, flat.k, flat.v, flat.k_scale, flat.v_scale), flat._tensors)
 
 
-def _keeping(desc, tensors):
-    desc._tensors = tensors
-    return desc
-
-
-def _rows(t: torch.Tensor) -> Heads:
-    """A [token, head, head_dim] view, any strides, head_dim dense."""
+def _rows(t: torch.Tensor, d: Optional[int] = None) -> Heads:
+    """A [token, head, head_dim] view on GPU d, any strides, head_dim dense."""
     st, sh, sd = t.stride()
-    if not t.is_cuda or (sd != 1 and t.shape[2] != 1):
-        raise ValueError("forge needs [token, head, head_dim] GPU tensors with a dense last axis")
+    if t.get_device() != d or (sd != 1 and t.shape[2] != 1):
+        _refuse(t.get_device(), d, "forge needs [token, head, head_dim] GPU tensors with a dense last axis")
     return Heads(t.data_ptr(), 0, st, sh)
 
 
 def forge_paged_append(cache: PagedCache, k, v, slots, rope=None, positions=None, q=None, q_out=None, layer=0):
     """k, v [T,Hkv,dh] views into the rows of slots [T], k rotated at positions [T]; q [T,Hq,dh] rotated into q_out (may be q)."""
-    T, heads, dh = k.shape
-    _here(k)
+    (T, heads, dh), d = k.shape, _device()
+    _here(cache, d)
+    if rope is not None:
+        _here(rope, d)
     if heads != cache.kv_heads or dh != cache.head_dim or v.shape != k.shape:
         raise ValueError("k and v must be [T, %d, %d]" % (cache.kv_heads, cache.head_dim))
     if (q is None) != (q_out is None) or slots is None:
@@ -726,21 +750,21 @@ def forge_paged_append(cache: PagedCache, k, v, slots, rope=None, positions=None
         if q.shape != (T, q_heads, dh) or q_out.shape != q.shape:
             raise ValueError("q and q_out must be [%d, Hq, %d]" % (T, dh))
         _cache_dt(cache, k, v, q, q_out)
-        qp, qop = C.byref(_rows(q)), C.byref(_rows(q_out))
-    _check(lib().forge_paged_append(C.byref(cache), layer, None if rope is None else C.byref(rope), C.byref(_rows(k)), C.byref(_rows(v)),
-                                    qp, qop, q_heads, _vector(slots, T, "slots"), None if positions is None else _vector(positions, T, "positions"), T,
-                                    _stream()), "forge_paged_append")
+        qp, qop = C.byref(_rows(q, d)), C.byref(_rows(q_out, d))
+    _check(lib().forge_paged_append(C.byref(cache), layer, None if rope is None else C.byref(rope), C.byref(_rows(k, d)), C.byref(_rows(v, d)),
+                                    qp, qop, q_heads, _vector(slots, T, "slots", d),
+                                    None if positions is None else _vector(positions, T, "positions", d), T, _stream(d)), "forge_paged_append")
 
 
 def forge_paged_read(cache: PagedCache, k_out, v_out, slots, layer=0):
     """k_out, v_out [T,Hkv,dh] views: the rows of slots [T] as values in the cache's activation type."""
-    T, heads, dh = k_out.shape
-    _here(k_out)
+    (T, heads, dh), d = k_out.shape, _device()
+    _here(cache, d)
     if (heads, dh) != (cache.kv_heads, cache.head_dim) or v_out.shape != k_out.shape or slots is None:
         raise ValueError("k_out and v_out must be [T, %d, %d]" % (cache.kv_heads, cache.head_dim))
     _cache_dt(cache, k_out, v_out)
-    _check(lib().forge_paged_read(C.byref(cache), layer, C.byref(_rows(k_out)), C.byref(_rows(v_out)), _vector(slots, T, "slots"), T,
-                                  _stream()), "forge_paged_read")
+    _check(lib().forge_paged_read(C.byref(cache), layer, C.byref(_rows(k_out, d)), C.byref(_rows(v_out, d)),
+                                  _vector(slots, T, "slots", d), T, _stream(d)), "forge_paged_read")
     return k_out, v_out
 
 
@@ -751,18 +775,18 @@ def forge_attn_paged_workspace_bytes(cache: PagedCache, q_heads, batch, max_len)
 def forge_attn_paged(cache: PagedCache, q, out, lengths, table, max_len, scale=None, workspace=None, layer=0):
     """q [B,Hq,dh] view; out [B,Hq*dh]; request b attends to its first lengths[b] rows (none: zeros), in the pages table[b] names."""
     B, H, dh = q.shape
-    if dh != cache.head_dim or out.shape != (B, H * dh) or lengths is None or table.dim() != 2:
+    if dh != cache.head_dim or out.shape != (B, H * dh) or lengths is None or table.dim() != 2 or table.shape[0] != B:
         raise ValueError("q must be [B, Hq, %d], out [B, Hq * %d], table [B, cols]" % (cache.head_dim, cache.head_dim))
     _cache_dt(cache, q, out)
-    sb, sh, sd = q.stride()
-    if not q.is_cuda or (sd != 1 and dh != 1):
-        raise ValueError("forge needs [request, head, head_dim] GPU tensors with a dense last axis")
-    _here(q)
+    (sb, sh, sd), d = q.stride(), _device()
+    _here(cache, d)
+    if q.get_device() != d or (sd != 1 and dh != 1):
+        _refuse(q.get_device(), d, "forge needs [request, head, head_dim] GPU tensors with a dense last axis")
     view = Heads(q.data_ptr(), sb, 0, sh)
-    wp, wb = _ws(workspace)
-    _check(lib().forge_attn_paged(C.byref(cache), layer, C.byref(view), _p(out), _vector(lengths, B, "lengths"),
-                                  _int32(table, (B, table.shape[1]), "table"), table.shape[1], H, B, max_len,
-                                  dh ** -0.5 if scale is None else scale, wp, wb, _stream()), "forge_attn_paged")
+    wp, wb = _ws_at(workspace, d)
+    _check(lib().forge_attn_paged(C.byref(cache), layer, C.byref(view), _at(out, d), _vector(lengths, B, "lengths", d),
+                                  _vector(table, B * table.shape[1], "table", d), table.shape[1], H, B, max_len,
+                                  dh ** -0.5 if scale is None else scale, wp, wb, _stream(d)), "forge_attn_paged")
     return out
 
 
@@ -784,15 +808,15 @@ def forge_adapters_workspace_bytes(adapters: Adapters, M) -> int:
 
 def forge_adapters_add(adapters: Adapters, x, base, y, ids, workspace=None):
     """y[m, :N] = base[m, :N] + the adapter ids[m] of x[m] (none where it is outside the range); y may be base, and both wider than N."""
-    M, K = x.shape
-    _here(x)
+    (M, K), d = x.shape, _device()
+    _here(adapters, d)
     if K != adapters.K or base.shape != y.shape or y.shape[0] != M or ids is None:
         raise ValueError("x must be [M, %d], base and y [M, at least %d]" % (adapters.K, adapters.N))
     if not x.dtype == base.dtype == y.dtype or _dt(x) != adapters.dt:
         raise ValueError("x, base, y and the adapters must agree in dtype")
-    wp, wb = _ws(workspace)
-    _check(lib().forge_adapters_add(C.byref(adapters), _p(x), _p(base), _p(y), _vector(ids, M, "ids"), M, y.shape[1], wp, wb, _stream()),
-           "forge_adapters_add")
+    wp, wb = _ws_at(workspace, d)
+    _check(lib().forge_adapters_add(C.byref(adapters), _at(x, d), _at(base, d), _at(y, d), _vector(ids, M, "ids", d), M, y.shape[1], wp, wb,
+                                    _stream(d)), "forge_adapters_add")
     return y
 
 
