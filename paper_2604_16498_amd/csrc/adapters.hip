@@ -8,11 +8,10 @@
 // of rank 16 beside q, k and v of 4096: 8 + 8 us for 19 + 10 MB of adapters).  The rows of x, base and y bound a prompt (4096 rows of 5 requests, rank 64,
 // 4096 x 4096: 15.8 + 21.3 us for 34 + 67 MB; one row of 768 in fp32 4.4 + 4.6).
 #include "paged.hpp"
+#include "adapters_plan.hpp"
 
 namespace forge {
 namespace {
-
-constexpr int JT = 4;          // 16-wide tiles of the inner index a block works on
 
 // Operands of 16 rows x 64 bytes: lane l has 16 bytes of row l % 16 at 16 (l / 16)
 template <typename T> struct Mma;
@@ -51,9 +50,6 @@ struct Rows {
     }
   }
 };
-
-// groups: of 64 columns, a block of the second launch
-struct Cut { int tiles, splits, chunks, lanes, groups; };
 
 // t of 16 RT rows and 64 inner columns over one range of K, in units of 512 bytes a row: a load of a block is 8 rows x 512 bytes (a kernel that only
 // read 4096 rows of 8 KB took 7.9 us so, 12.0 in lines of 128 bytes), two units of x and of the adapter are on their way in registers, and a unit
@@ -467,87 +463,41 @@ __global__ __launch_bounds__(256, 2) void adapters_outer_many_kernel(AdapterArgs
   }
 }
 
-// Whether blocks take 64 rows, most of which share an adapter with their neighbours: where their tiles of 64 rows and 256 columns, and in the first launch
-// 64 rows and 64 inner columns, are enough.  bf16, 64 rows | 16, us: 768 x 768, rank 64, 1500 rows (69 tiles) 14.2 | 14.0, 4096 (192) 15.5 | 18.7; 4096 x 4096,
-// rank 64, 512 rows (128, 8 in the first launch) 18.6 | 17.0, 1000 20.9 | 22.4, 4096 36.6 | 50.4; beside q, k and v (192, 24) 24.5 | 28.0.  In fp32 a block's
-// chain of matrix instructions is 8 times as long: 2304 x 768, rank 64, 1500 rows (207 tiles) 36.1 | 35.6, 4096 (576) 61.5 | 71.1; rank 8 17.9 | 16.3 and
-// 30.1 | 31.4.
-constexpr int MANY = 512;
-bool many_rows(int M, int N, int inner, forge_dtype dt) {
-  const int64_t tiles = (int64_t)(M / 64) * ceil_div(N, 256);
-  return M >= MANY && (int64_t)M * ceil_div(inner, 16 * JT) >= 900 && tiles >= (dt == FORGE_BF16 ? 72 : 256);
-}
-
-// Blocks beside one another that deal a tile's adapters, of which 16 rows have at most 16, where there are few tiles: as many as are resident at once (a
-// tile of a prompt has one adapter, and what more there are pass over it in turn; 3 | 8 per CU in both launches, 4096 x 4096, us: 500 rows of 5 requests,
-// rank 64, 16.9 | 19.6; 256 requests of rank 8 20.0 | 26.1)
-int lanes_of(int64_t blocks, int rows) {
-  const int64_t l = ceil_div64(3 * compute_units(), blocks);
-  const int most = rows < 16 ? rows : 16;
-  return (int)(l < 1 ? 1 : l < most ? l : most);
-}
-
-// K in ranges until the blocks fill the chip twice (of many rows once: 4096 x 4096, rank 64, 4 | 8 ranges 15.2 | 15.6 us, and less to add up)
-Cut cut_of(int M, int K, int inner, bool many, forge_dtype dt) {
-  const int units = ceil_div(K, dt == FORGE_BF16 ? 256 : 128);
-  Cut c;
-  c.tiles = ceil_div(M, many ? 64 : 16);
-  c.chunks = ceil_div(inner, 16 * JT);
-  const int64_t blocks = (int64_t)c.tiles * c.chunks;
-  const int want = (int)ceil_div64((many ? 1 : 2) * compute_units(), blocks);
-  const int most = many ? units : ceil_div(units, 2);     // (two units a block: both are on their way at once)
-  c.splits = want < most ? want : most;
-  c.lanes = c.groups = 1;
-  return c;
-}
-
-// whether the columns are whole blocks of the second launch for many rows
-bool whole_blocks(const AdapterArgs& a) {
-  bool whole = a.ldy % 4 == 0;
-  for (int i = 0; i < a.parts; ++i) whole = whole && a.part_end[i] % 256 == 0;
-  return whole;
-}
-
 template <typename T, int NS>
 forge_status launch_outer(const AdapterArgs& a, Cut c, bool many, hipStream_t s) {
-  if (many && whole_blocks(a)) {
+  if (many && adapters_whole(a.ldy, a.parts, a.part_end)) {
     adapters_outer_many_kernel<T, NS><<<(unsigned)(ceil_div(ceil_div(a.M, 64), 8) * 8 * (a.N / 256)), 256, 0, s>>>(a, c);
     return launch_status();
   }
   c.groups = a.N <= 256 ? 4 : 8;
   const int64_t blocks = (int64_t)ceil_div(a.M, 16) * ceil_div(a.N, 64 * c.groups);
-  c.lanes = lanes_of(blocks, a.M);
+  c.lanes = adapters_lanes(blocks, a.M, compute_units());
   adapters_outer_kernel<T, NS><<<dim3((unsigned)blocks, c.lanes), 256, 0, s>>>(a, c);
   return launch_status();
 }
 template <typename T>
 forge_status launch(const AdapterArgs& a, hipStream_t s) {
+  constexpr bool F32 = sizeof(T) == 4;
   const int inner = a.parts * a.rank;
-  const bool many = many_rows(a.M, a.N, inner, a.dt);
-  Cut c = cut_of(a.M, a.K, inner, many, a.dt);
-  c.lanes = many ? 2 : lanes_of((int64_t)c.tiles * c.chunks * c.splits, a.M);
+  const bool many = adapters_many(a.M, a.N, inner, F32);
+  const Cut c = adapters_cut(a.M, a.K, inner, many, F32, compute_units());
   const dim3 grid(c.tiles, c.chunks * c.splits, c.lanes);
   if (many) adapters_inner_kernel<T, 4><<<grid, 256, 0, s>>>(a, c);
   else adapters_inner_kernel<T, 1><<<grid, 256, 0, s>>>(a, c);
   if (hipGetLastError() != hipSuccess) return FORGE_ERR_HIP;
-  const int steps = ceil_div(a.rank, Mma<T>::STEP);
+  const int steps = adapters_steps(a.rank, F32);
   if (steps == 1) return launch_outer<T, 1>(a, c, many, s);
   if (steps == 2) return launch_outer<T, 2>(a, c, many, s);
-  if constexpr (sizeof(T) == 4) {
-    if (steps > 4) return launch_outer<T, 8>(a, c, many, s);
+  if constexpr (F32) {
+    if (steps == 8) return launch_outer<T, 8>(a, c, many, s);
   }
   return launch_outer<T, 4>(a, c, many, s);
 }
 
 }  // namespace
 
-// Room for any smaller M too: of m rows in `tiles` tiles the ranges are at most the units of K, and at most 2 cus (1 of 64 rows) / (tiles chunks) + 1; times m rows, of
-// which a tile has at most 16 or 64
-size_t adapters_workspace_bytes(int M, int N, int K, int rank, int parts, forge_dtype dt) {
-  const int inner = parts * rank, units = ceil_div(K, dt == FORGE_BF16 ? 256 : 128);
-  const int64_t most = (int64_t)units * M;
-  const int64_t full = ceil_div((M >= MANY ? 64 : 32) * compute_units(), ceil_div(inner, 16 * JT)) + (int64_t)M;
-  return (size_t)(most < full ? most : full) * inner * sizeof(float);
+size_t adapters_workspace_bytes(int M, int K, int rank, int parts, forge_dtype dt) {
+  return adapters_room(M, K, parts * rank, dt == FORGE_F32, compute_units());
 }
 
 forge_status launch_adapters(const AdapterArgs& a, hipStream_t s) {

@@ -54,6 +54,6 @@ struct AdapterArgs {
   void* workspace;
 };
 forge_status launch_adapters(const AdapterArgs& a, hipStream_t s);
-size_t adapters_workspace_bytes(int M, int N, int K, int rank, int parts, forge_dtype dt);
+size_t adapters_workspace_bytes(int M, int K, int rank, int parts, forge_dtype dt);
 
 }  // namespace forge

@@ -187,7 +187,7 @@ forge_status forge_attn_paged(const forge_paged_cache* cache, int layer, const f
 
 size_t forge_adapters_workspace_bytes(const forge_adapters* d, int M) {
   if (check_adapters(d) != FORGE_OK || M < 1 || !gemm_size_ok(M, d->N)) return 0;
-  return adapters_workspace_bytes(M, d->N, d->K, d->rank, d->n_parts, d->dt);
+  return adapters_workspace_bytes(M, d->K, d->rank, d->n_parts, d->dt);
 }
 
 forge_status forge_adapters_add(const forge_adapters* d, const void* x, const void* base, void* y, const int32_t* ids, int M,
@@ -198,7 +198,7 @@ forge_status forge_adapters_add(const forge_adapters* d, const void* x, const vo
     return FORGE_ERR_INVALID_ARG;
   if (ldy != 0 && ldy < d->N) return FORGE_ERR_INVALID_ARG;
   if (!gemm_size_ok(M, d->N) || ldy > kMaxRows) return FORGE_ERR_UNSUPPORTED;
-  const size_t need = adapters_workspace_bytes(M, d->N, d->K, d->rank, d->n_parts, d->dt);
+  const size_t need = adapters_workspace_bytes(M, d->K, d->rank, d->n_parts, d->dt);
   if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return FORGE_ERR_WORKSPACE;
   const AdapterArgs a = {d->a, d->b, d->scale, x, base, y, ids, M, d->N, d->K, d->n_adapters, d->rank, d->n_parts,
                          ldy == 0 ? d->N : ldy, {d->part_end[0], d->part_end[1], d->part_end[2], d->part_end[3]}, d->dt, workspace};
