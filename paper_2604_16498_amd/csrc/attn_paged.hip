@@ -15,6 +15,7 @@
 // loads (length, pages, three tiles).  Registers: 168 for 8-bit rows, 208 for 16-bit heads of 128, no spills.
 #include "cache_tiles.hpp"
 #include "paged.hpp"
+#include "paged_plan.hpp"
 
 namespace forge {
 namespace {
@@ -331,20 +332,14 @@ void launch_merge(const PagedParams& p, int head_dim, hipStream_t s) {
 
 }  // namespace
 
-// Room for the shares of any smaller batch and shorter request: their number only falls with either.
 size_t attn_paged_workspace_bytes(int batch, int q_heads, int kv_heads, int head_dim, int max_len) {
-  const int most = kMaxPairs / kv_heads < MAX_DEALT ? kMaxPairs / kv_heads : MAX_DEALT;
-  const int64_t pairs = (int64_t)(batch < most ? batch : most) * kv_heads;
-  if (max_len <= MIN_CUT_ROWS) return 0;
-  const int shares = tree_shares(pairs, max_len, 1, 2, compute_units());
-  return (size_t)shares * ceil_div(q_heads / kv_heads, 16) * 2 * 16 * (head_dim + 2) * sizeof(float);
+  return paged_room(batch, q_heads, kv_heads, head_dim, max_len, compute_units());
 }
 
 forge_status launch_attn_paged(const PagedAttnArgs& a, hipStream_t s) {
   const bool f32 = a.dt == FORGE_F32;
   const int group = a.q_heads / a.kv_heads, cus = compute_units();
-  const TreePlan pl = plan_tree(a.batch, a.kv_heads * (group < 16 ? group : 16), a.kv_heads, a.head_dim, 1, a.max_len,
-                                1 << 30, a.type != FORGE_KV_SAME ? 1 : f32 ? 4 : 2, true, cus);
+  const TreePlan pl = plan_paged(a.batch, a.q_heads, a.kv_heads, a.head_dim, a.max_len, a.type != FORGE_KV_SAME ? 1 : f32 ? 4 : 2, cus);
   PagedParams p;
   p.c = a.cache.c;
   p.q = a.q;
@@ -363,7 +358,7 @@ forge_status launch_attn_paged(const PagedAttnArgs& a, hipStream_t s) {
   p.max_len = a.max_len;
   p.shares = pl.shares;
   p.dealt = pl.dealt;
-  p.row_blocks = ceil_div(group, 16);
+  p.row_blocks = pl.row_blocks;
   const int apart = pl.each ? NW : 1;
   const int64_t each_blocks = ceil_div(pl.shares, apart);
   p.by_length = !pl.dealt && a.batch > 1 && a.batch <= 64 && each_blocks * p.row_blocks > cus && p.row_blocks <= cus ? cus / p.row_blocks * apart : 0;

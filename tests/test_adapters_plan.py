@@ -1,5 +1,5 @@
 """Which kernels and which cut the adapters take (the library's own source, built for the host): that the calls of adapter_plan_cases.py take what is
-listed there and leave out nothing."""
+listed there and leave out nothing, and that the workspace holds what the first launch writes."""
 import ctypes as C
 import os
 import shutil
@@ -25,6 +25,17 @@ extern "C" void plan(int M, int K, int parts, const int* ends, int rank, int ldy
   o[0] = many ? 64 : 16; o[1] = many && adapters_whole(ldy, parts, ends) ? 64 : 16; o[2] = adapters_steps(rank, f32);
   o[3] = c.splits; o[4] = c.tiles; o[5] = c.chunks; o[6] = c.lanes;
 }
+extern "C" size_t room(int M, int K, int inner, int f32, int cus) { return adapters_room(M, K, inner, f32, cus); }
+// the first of m = 1 .. M rows whose t of all ranges has no room in the workspace of M rows, 0 where there is none
+extern "C" int first_without_room(int M, int K, int N, int parts, int rank, int f32, int cus) {
+  const int inner = parts * rank;
+  const size_t have = adapters_room(M, K, inner, f32, cus);
+  for (int m = 1; m <= M; ++m) {
+    const Cut c = adapters_cut(m, K, inner, adapters_many(m, N, inner, f32), f32, cus);
+    if ((size_t)c.splits * m * inner * sizeof(float) > have) return m;
+  }
+  return 0;
+}
 """
 
 
@@ -35,7 +46,9 @@ def host(tmp_path_factory):
     d = tmp_path_factory.mktemp("plan")
     (d / "shim.cpp").write_text(SHIM % os.path.join(build.CSRC, "adapters_plan.hpp"))
     subprocess.run(["g++", "-O2", "-shared", "-fPIC", str(d / "shim.cpp"), "-o", str(d / "shim.so")], check=True)
-    return C.CDLL(str(d / "shim.so"))
+    lib = C.CDLL(str(d / "shim.so"))
+    lib.room.restype = C.c_size_t
+    return lib
 
 
 def ask(host, dt, M, K, ends, rank, ldy, cus=256):
@@ -55,6 +68,18 @@ def test_cases_take_what_is_listed(host, dt):
 def test_cases_leave_nothing_out(host, dt):
     steps = (1, 2, 4) if dt == "bf16" else (1, 2, 4, 8)
     assert {w for _, w in CASES[dt]} == {(a, b, s) for a, b in ((64, 64), (64, 16), (16, 16)) for s in steps}
+
+
+# ends of the range of every argument that the sizes depend on; few and many compute units
+@pytest.mark.parametrize("cus", [1, 64, 256, 304])
+@pytest.mark.parametrize("dt", list(CASES))
+def test_a_workspace_holds_what_is_written_for_it_and_every_smaller_call(host, dt, cus):
+    for K in (8, 768, 4096, 14336):
+        for N in (16, 768, 4096, 28672):
+            for rank, parts in ((8, 1), (16, 3), (64, 1), (128, 4)):
+                for M in (1, 7, 16, 100, 511, 512, 513, 1500, 4100):
+                    m = host.first_without_room(M, K, N, parts, rank, dt == "fp32", cus)
+                    assert m == 0, (K, N, rank, parts, M, m)
 
 
 @pytest.mark.parametrize("dt", list(CASES))
