@@ -434,7 +434,8 @@ forge_status forge_kv_append(const forge_kv_cache* cache, int layer, const forge
                              const int32_t* seq_pos, const int32_t* positions, int n, int max_pos, void* stream);
 
 /* Rows seq_pos[b] .. seq_pos[b] + n - 1 (seq_pos NULL: max_pos .., 0 for the first n) of layer `layer`, as the values they stand
- * for, rounded once to dt: k_out, v_out [batch, kv_heads, n, head_dim] dense, what forge_attn_fused takes. */
+ * for (8 bits: code times scale, rounded to fp32 and then to dt): k_out, v_out [batch, kv_heads, n, head_dim] dense, what
+ * forge_attn_fused takes. */
 forge_status forge_kv_read(const forge_kv_cache* cache, int layer, void* k_out, void* v_out, const int32_t* seq_pos, int n,
                            int max_pos, void* stream);
 
@@ -522,8 +523,8 @@ forge_status forge_paged_append(const forge_paged_cache* cache, int layer, const
                                 const forge_heads* v, const forge_heads* q, const forge_heads* q_out, int q_heads,
                                 const int32_t* slots, const int32_t* positions, int tokens, void* stream);
 
-/* The rows in slots[0 .. tokens - 1] of layer `layer`, as the values they stand for, rounded once to dt, into [token, head, head_dim] views (head-major
- * ones, as forge_attn_fused takes them, among them; their batch_stride is not looked at).  Slots may repeat.  A token whose slot is
+/* The rows in slots[0 .. tokens - 1] of layer `layer`, as the values they stand for (8 bits: code times scale, rounded to fp32 and then to dt), into
+ * [token, head, head_dim] views (head-major ones, as forge_attn_fused takes them, among them; their batch_stride is not looked at).  Slots may repeat.  A token whose slot is
  * outside the pool is left out: its rows of k_out and v_out stay as they were. */
 forge_status forge_paged_read(const forge_paged_cache* cache, int layer, const forge_heads* k_out, const forge_heads* v_out,
                               const int32_t* slots, int tokens, void* stream);
@@ -536,7 +537,8 @@ forge_status forge_paged_read(const forge_paged_cache* cache, int layer, const f
  * row are not used.  What lies in rows behind a length, infinities and NaN among it, does not reach the output; an infinity in a row of v
  * before it does, however small the row's weight (of a finite score; it is positive).
  * q: [batch, head, head_dim] view (its token_stride is not looked at); out: [batch, q_heads * head_dim] dense, in dt.  fp32 scores, statistics and
- * sums; for bf16 the weights are rounded to bf16 for the second product.  q_heads a multiple of kv_heads; (batch * kv_heads + 8) times the sixteens of
+ * sums; for bf16 the weights are rounded for the second product, to two bf16 parts (16 bits) with up to 8 query heads a cache head, to bf16 with more.
+ * A max_len above all lengths to come, as a recorded step needs it, costs a few us more (64 requests: 3 at 32768).  q_heads a multiple of kv_heads; (batch * kv_heads + 8) times the sixteens of
  * q_heads / kv_heads stay below 2^24.  The workspace size serves every smaller max_len and batch too. */
 size_t forge_attn_paged_workspace_bytes(const forge_paged_cache* cache, int q_heads, int batch, int max_len);
 forge_status forge_attn_paged(const forge_paged_cache* cache, int layer, const forge_heads* q, void* out, const int32_t* lengths,

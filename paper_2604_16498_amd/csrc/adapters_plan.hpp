@@ -16,6 +16,11 @@ struct Cut { int tiles, splits, chunks, lanes, groups; };
 // rank 64, 512 rows (128, 8 in the first launch) 18.6 | 17.0, 1000 20.9 | 22.4, 4096 36.6 | 50.4; beside q, k and v (192, 24) 24.5 | 28.0.  In fp32 a block's
 // chain of matrix instructions is 8 times as long: 2304 x 768, rank 64, 1500 rows (207 tiles) 36.1 | 35.6, 4096 (576) 61.5 | 71.1; rank 8 17.9 | 16.3 and
 // 30.1 | 31.4.
+// The adapter numbers lie on the device, so the rule cannot see a batch whose neighbours have different adapters: a block then works through up to 64 of them in
+// turn, with 16 rows at most 16, dealt over more blocks.  4096 x 4096, row m with adapter m mod n, us: 1024 rows, rank 8, n = 8 25.7 | 31.3, 16 43.7 | 56.0,
+// 24 64.6 | 55.2, 64 159 | 56.7, 1024 160 | 63.4; rank 64, 16 63.6 | 136, 32 110 | 136, 64 204 | 137, 512 233 | 183; 2048 rows, rank 8, 2048 249 | 125, rank 64,
+// 512 318 | 293; fp32, 1024 rows, rank 8, 16 100 | 117, 64 369 | 119.  In runs of 16 rows, 1024 rows, rank 8 17.0 | 12.1, rank 64 29.8 | 24.4.  So the larger
+// tiles gain up to about 20 adapters that alternate, and decode batches of more than 900 requests with one each lose by them.
 constexpr int MANY = 512;
 inline bool adapters_many(int M, int N, int inner, bool f32) {
   const int64_t tiles = (int64_t)(M / 64) * ceil_div(N, 256);

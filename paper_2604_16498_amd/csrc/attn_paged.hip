@@ -9,10 +9,18 @@
 // A weight is positive, however far its row lies below the maximum: an infinity in that row of v counts.  So weights, the running rescaling and the
 // waves' and shares' parts do not become 0 where fp32 would round them to it; what that adds to a finite sum is 2^-133 of its rows of v.
 // What is its own is where a tile lies: in two halves of 16 rows, each inside a page, whose numbers a wave keeps in a
-// register, an entry a lane, for its next 32 tiles; a half's address is then scalar arithmetic.  A row is read once and goes past the caches.
-// Measured, 32 heads over 8 of 128: 64 requests up to 2049 rows, int8 (164 MB) 33.6 us, 4.9 TB/s (rows through the caches 37.0), two blocks a CU of uneven
-// lengths; 7 up to 30011 rows, bf16 (430 MB) 69.4 us, 6.2 TB/s, and 4.7 for the merge (77 + 4.7).  One of 334 rows of 12 heads of 64: 5.8 us, a chain of
-// loads (length, pages, three tiles).  Registers: 168 for 8-bit rows, 208 for 16-bit heads of 128, no spills.
+// register, an entry a lane, for its next 32 tiles; a half's address is then scalar arithmetic.  Rows are asked for past the caches: up to 16 query heads a cache
+// head they are read once.  (With more each block of 16 reads them, those of a share beside one another on one XCD; 40 over 1 of 128, 16 up to 8192 rows,
+// bf16, 42 MB: 26.3 us, 1.6 TB/s.)
+// Measured, 32 heads over 8 of 128: 64 requests up to 2049 rows, int8 (164 MB) 33.5 us, 4.9 TB/s (rows through the caches 37.0), two blocks a CU of uneven
+// lengths; 7 up to 30011 rows, bf16 (430 MB) 67 to 69 us, 6.2 to 6.4 TB/s, and 4.6 for the merge (through the caches 77).  One of 334 rows of 12 heads of
+// 64: 6.0 us, 5.2 in a graph, a chain of loads (length, pages, three tiles).  fp32, 12 heads of 64, 8 up to 1000 rows (31 MB) 16.4 us: in fp32 the cut's
+// speeds are those of the drafted trees' kernel, not fitted here, and heads of 128 hold 134 KB of LDS, one block a CU where the cut counts on two.
+// max_len far above the lengths, as a recorded step has it (the cut is then made for that): 64 up to 2048 rows, bf16, max_len 2048 54.6, 32768 55.1,
+// 131072 60.0; int8 33.3, 36.6, 36.9; 64 up to 300 rows, int8, 300 11.5, 4096 11.8, 32768 14.6; 8 up to 4096, bf16, 4096 to 131072 20.2 to 21.0; one of 334
+// 5.1, from 4096 on 7.9 (the merge's launch).
+// Registers: 162 for 8-bit and 216 for 16-bit heads of 128, 117 to 140 for heads of 64; fp32 162, 251 and 40 accumulation registers.  Up to 9 scalar ones of
+// the 8-bit kernels are spilled into vector registers, no others.
 #include "cache_tiles.hpp"
 #include "paged.hpp"
 #include "paged_plan.hpp"
